@@ -277,6 +277,85 @@ ds_status_t ds_server_aggregate_compress_update(ds_ctx_t *ctx, uint64_t step, co
                                                 float *delta_s, const ds_payload_t *out, float *x,
                                                 float *m, float gamma, float beta, void *hip_stream);
 
+/* Orthogonalised updates: Newton-Schulz products.
+ *
+ * A plan (ds_ortho_t) names the matrices of a model's flat vector of d elements.  For a matrix U [rows, cols]:
+ *   X = U / (||U||_F + eps), transposed if rows > cols ; `steps` times, with that step's a, b, c:
+ *   G = X X' ; X <- a X + (b G + c G G) X ;  O(U) = factor * X, transposed back
+ * which draws the singular values of U towards one (Muon's update).  A matrix of zeros gives zeros (also with
+ * eps = 0).  Element (i, j) of a matrix is element offset + i * ld + j of the vector; matrices may have any size,
+ * offset and row stride (column blocks of one wider array are matrices with its row length as their ld) but no
+ * element may belong to two of them.  Elements in no matrix are not read and not written.
+ *
+ * Products: operands are held as the sum of two halves of 11 bits (three matrix products, sums in fp32), so results are
+ * as those of fp32 products; with DS_ORTHO_HALF as one half of 11 bits (one product, a third of the time), for results that
+ * are kept in bf16 or need no more.  Both are scaled by powers of two, so small entries keep their bits.  Norms are
+ * summed in fp64.  The iteration must not let singular values grow beyond 2: every list of coefficients that
+ * converges for singular values in [0, 1] does not.  Sums are taken in a fixed order: equal calls give equal bits. */
+typedef struct {
+    int64_t offset;           /* of element (0, 0) in the vector */
+    int64_t ld;               /* elements between rows, >= cols (0: cols) */
+    int32_t rows, cols;       /* >= 1; the smaller of the two at most 32768, the larger at most 2^24 */
+} ds_matrix_t;
+
+typedef enum {
+    DS_ORTHO_FACTOR_NONE = 0,   /* 1 */
+    DS_ORTHO_FACTOR_ASPECT = 1, /* sqrt(max(1, rows / cols)) */
+    DS_ORTHO_FACTOR_RMS = 2     /* 0.2 * sqrt(max(rows, cols)): entries of the size that AdamW's have */
+} ds_ortho_factor_t;
+
+typedef enum {
+    DS_ORTHO_NESTEROV = 1,    /* ds_apply_update_ortho: orthogonalise beta m + q instead of m */
+    DS_ORTHO_HALF = 2         /* one product of half precision instead of three */
+} ds_ortho_flags_t;
+
+typedef struct {
+    int64_t d;                /* elements of the vector, 1 .. 2^31-1 */
+    const ds_matrix_t *mats;  /* HOST array of n_mats; copied by ds_ortho_create */
+    int32_t n_mats;           /* 1 .. 2^20 */
+    int32_t steps;            /* 1 .. 32 */
+    const float *coef;        /* HOST array [steps][3] of a, b, c, copied; NULL: 3.4445, -4.7750, 2.0315 in every step */
+    float eps;                /* >= 0 */
+    int32_t factor;           /* ds_ortho_factor_t */
+    int32_t flags;            /* ds_ortho_flags_t bits */
+} ds_ortho_config_t;
+
+typedef struct ds_ortho ds_ortho_t;
+
+/* Creates a plan on the current device with its tables and its workspace (4 bytes per element of the vector and about 12 per
+ * element of the matrices, half of that with DS_ORTHO_HALF, each matrix's sides rounded up to the tiles of its kernels).  Errors: NULL, SHAPE (d, n_mats, steps or a matrix out of range), CONFIG (bad
+ * enum or flag, eps or a coefficient negative or not finite where it must not be, two matrices that share an element), DEVICE.
+ * Calls with one plan share its workspace: they must not overlap (one stream, or ordered by events; that holds for
+ * replays of captured graphs too). */
+ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out);
+
+/* Frees the plan.  The caller must have synchronised the streams that used it.  NULL is accepted. */
+ds_status_t ds_ortho_destroy(ds_ortho_t *plan);
+
+/* dst <- O(src), for every matrix of the plan.  src, dst: vectors of d elements, each DS_F32 or DS_BF16, 16-byte
+ * aligned; dst may be src if the types agree, and must not overlap it otherwise. */
+ds_status_t ds_orthogonalize(ds_ortho_t *plan, const void *src, int32_t src_dtype, void *dst, int32_t dst_dtype,
+                             void *hip_stream);
+
+/* Model update from the server's message `srv` through the plan's matrices, q = decode(srv), on their elements only:
+ *   m <- fma(beta, m, q) ; u = m, or fma(beta, m, q) with DS_ORTHO_NESTEROV   (m == NULL: u = q)
+ *   x <- (1 - gamma * decay) x - gamma O(u)
+ * x, m: [d] fp32, in place.  The context and the plan must be of the same d and device (DS_ERR_SHAPE, DS_ERR_CONFIG).
+ * Any compressor (TERNARY's server message is the dense average). */
+ds_status_t ds_apply_update_ortho(ds_ctx_t *ctx, ds_ortho_t *plan, const ds_payload_t *srv, float *x, float *m, float gamma,
+                                  float beta, float decay, void *hip_stream);
+
+/* Model update from the server's message by AdamW, on every element or, with a plan, on those in none of its matrices:
+ *   m <- beta1 m + (1 - beta1) q ; v <- beta2 v + (1 - beta2) q^2
+ *   x <- (1 - gamma * decay) x - gamma (m / (1 - beta1^(step+1))) / (sqrt(v / (1 - beta2^(step+1))) + eps)
+ * `step` counts from 0; a captured graph keeps the step of its capture.  The constants are doubles because 1 - beta2 is
+ * not the difference of two floats: 1 - 0.999f is 1.3e-5 off.  0 <= beta1, beta2 < 1, eps >= 0 (else DS_ERR_CONFIG);
+ * where eps = 0 and v = 0 the quotient is 0 / 0.  x, m, v: [d] fp32, in place; v >= 0.  The plan is only read: calls of this
+ * kind may overlap with others that use it. */
+ds_status_t ds_apply_update_adamw(ds_ctx_t *ctx, const ds_ortho_t *skip, const ds_payload_t *srv, uint64_t step, float *x,
+                                  float *m, float *v, double gamma, double beta1, double beta2, double eps, double decay,
+                                  void *hip_stream);
+
 /* Decodes message `row` of a batch of `rows` messages into dense_out [d] (fp32): the
  * decoder of Q[.] that the server and the update use. */
 ds_status_t ds_decompress(ds_ctx_t *ctx, const ds_payload_t *p, int32_t rows, int32_t row,

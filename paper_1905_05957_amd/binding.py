@@ -25,6 +25,9 @@ FLAG_SERVER_IDENTITY = 16
 
 _COMP = {"identity": COMP_IDENTITY, "sign": COMP_SIGN, "topk": COMP_TOPK, "qsgd": COMP_QSGD,
          "clip": COMP_CLIP, "rsparse": COMP_RSPARSE, "ternary": COMP_TERNARY}
+ORTHO_FACTOR_NONE, ORTHO_FACTOR_ASPECT, ORTHO_FACTOR_RMS = 0, 1, 2
+ORTHO_NESTEROV, ORTHO_HALF = 1, 2
+_FACTOR = {"none": ORTHO_FACTOR_NONE, "aspect": ORTHO_FACTOR_ASPECT, "rms": ORTHO_FACTOR_RMS}
 _MODE = {"whole": SCALE_WHOLE, "segments": SCALE_SEGMENTS, "chunk": SCALE_CHUNK}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -45,6 +48,15 @@ class ds_config_t(C.Structure):
                 ("seed", C.c_uint64), ("topk_max_workgroups", C.c_int32), ("topk_spin_limit", C.c_int32)]
 
 
+class ds_matrix_t(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("ld", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32)]
+
+
+class ds_ortho_config_t(C.Structure):
+    _fields_ = [("d", C.c_int64), ("mats", C.POINTER(ds_matrix_t)), ("n_mats", C.c_int32), ("steps", C.c_int32),
+                ("coef", C.POINTER(C.c_float)), ("eps", C.c_float), ("factor", C.c_int32), ("flags", C.c_int32)]
+
+
 class ds_payload_t(C.Structure):
     _fields_ = [("sign_words", C.c_void_p), ("scales", C.c_void_p), ("levels", C.c_void_p),
                 ("pairs", C.c_void_p), ("dense", C.c_void_p)]
@@ -53,6 +65,7 @@ class ds_payload_t(C.Structure):
 EXPORTS = ["ds_create", "ds_destroy", "ds_payload_sizes", "ds_worker_compress",
            "ds_server_aggregate_compress", "ds_apply_update", "ds_decompress", "ds_materialize_error",
            "ds_server_aggregate_compress_update", "ds_worker_compress_sign_noalloc", "ds_status", "ds_probe_copy",
+           "ds_ortho_create", "ds_ortho_destroy", "ds_orthogonalize", "ds_apply_update_ortho", "ds_apply_update_adamw",
            "ds_status_string", "ds_version"]
 
 _lib = None
@@ -85,6 +98,11 @@ def load_library():
     L.ds_materialize_error.argtypes = [vp, vp, i64, vp, vp]
     L.ds_server_aggregate_compress_update.argtypes = [vp, u64, C.POINTER(ds_payload_t), vp, C.POINTER(ds_payload_t),
                                                       vp, vp, f32, f32, vp]
+    L.ds_ortho_create.argtypes = [C.POINTER(ds_ortho_config_t), C.POINTER(vp)]
+    L.ds_ortho_destroy.argtypes = [vp]
+    L.ds_orthogonalize.argtypes = [vp, vp, i32, vp, i32, vp]
+    L.ds_apply_update_ortho.argtypes = [vp, vp, C.POINTER(ds_payload_t), vp, vp, f32, f32, f32, vp]
+    L.ds_apply_update_adamw.argtypes = [vp, vp, C.POINTER(ds_payload_t), u64, vp, vp, vp, *[C.c_double] * 5, vp]
     L.ds_status.argtypes = [vp]
     L.ds_probe_copy.argtypes = [vp, vp, C.c_size_t, vp]
     L.ds_worker_compress_sign_noalloc.argtypes = [i32, i64, i32, i32, vp, i64, vp, i64, vp, vp, vp]
@@ -145,10 +163,16 @@ def _need(t: torch.Tensor, what: str, dtype, shape) -> torch.Tensor:
     return t
 
 
-def _stream_ptr(stream) -> Optional[int]:
+def _stream_ptr(stream, device=None) -> Optional[int]:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        stream = torch.cuda.current_stream(device)
     return C.c_void_p(stream.cuda_stream)
+
+
+def _one_device(device, **tensors) -> None:
+    for what, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{what}: on {t.device}, expected {device}")
 
 
 class Payload:
@@ -360,6 +384,43 @@ class Context:
                                               None if m is None else m.data_ptr(), gamma, beta,
                                               _stream_ptr(stream)), "ds_apply_update")
 
+    def _same_vector(self, plan: "OrthoPlan") -> "OrthoPlan":
+        if not isinstance(plan, OrthoPlan) or plan._h.value is None:
+            raise ValueError("plan: an open OrthoPlan is required")
+        if plan.d != self.d:
+            raise ValueError(f"plan: made for a vector of {plan.d} elements, the context for {self.d}")
+        return plan
+
+    def apply_update_ortho(self, plan: "OrthoPlan", srv: Payload, x: torch.Tensor, m: Optional[torch.Tensor], gamma: float,
+                           beta: float = 0.0, decay: float = 0.0, stream=None):
+        """The model update through the plan's matrices: momentum, orthogonalisation, weights.  Elements outside them stay."""
+        self._same_vector(plan)
+        _need(x, "x", torch.float32, (self.d,))
+        if m is not None:
+            _need(m, "m", torch.float32, (self.d,))
+        s = srv.check(self, 1, "srv", server=True)
+        _one_device(plan.device, x=x, m=m, **s.tensors())
+        s = s.c_struct()
+        _check(load_library().ds_apply_update_ortho(self._h, plan._h, C.byref(s), x.data_ptr(), None if m is None else m.data_ptr(),
+                                                    gamma, beta, decay, _stream_ptr(stream, plan.device)), "ds_apply_update_ortho")
+
+    def apply_update_adamw(self, srv: Payload, step: int, x: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gamma: float,
+                           beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, decay: float = 0.0,
+                           skip: Optional["OrthoPlan"] = None, stream=None):
+        """The model update by AdamW, on every element or on those outside the matrices of `skip`; `step` counts from 0."""
+        if skip is not None:
+            self._same_vector(skip)
+        for t, what in ((x, "x"), (m, "m"), (v, "v")):
+            _need(t, what, torch.float32, (self.d,))
+        if int(step) < 0:
+            raise ValueError("step: counts from 0")
+        s = srv.check(self, 1, "srv", server=True)
+        _one_device(x.device if skip is None else skip.device, x=x, m=m, v=v, **s.tensors())
+        s = s.c_struct()
+        _check(load_library().ds_apply_update_adamw(self._h, None if skip is None else skip._h, C.byref(s), int(step), x.data_ptr(),
+                                                    m.data_ptr(), v.data_ptr(), gamma, beta1, beta2, eps, decay,
+                                                    _stream_ptr(stream, x.device)), "ds_apply_update_adamw")
+
     def materialize_error(self, delta: Optional[torch.Tensor], delta_s: Optional[torch.Tensor],
                           stream=None):
         if delta is not None:
@@ -380,6 +441,70 @@ class Context:
         s = p.check(self, p.rows, "p", server=(self.server_identity and p.comp == COMP_IDENTITY)).c_struct()
         _check(load_library().ds_decompress(self._h, C.byref(s), p.rows, row, out.data_ptr(),
                                             _stream_ptr(stream)), "ds_decompress")
+
+
+class OrthoPlan:
+    """The matrices of a flat vector of d elements, to be orthogonalised by Newton-Schulz products (ds_ortho_t), on the
+    current device.
+
+    mats: (offset, rows, cols) or (offset, rows, cols, row stride) of each matrix; coef: (a, b, c) for every step, or a list
+    of one such triple per step; scale: "none", "aspect" or "rms", the factor of an orthogonalised matrix; half: products of half precision, a third of the time.
+    """
+
+    def __init__(self, d: int, mats, steps: int = 5, coef=None, eps: float = 1e-7, scale="none", nesterov: bool = False,
+                 half: bool = False):
+        L = load_library()
+        rows = [tuple(int(v) for v in m) for m in mats]
+        if any(len(m) not in (3, 4) for m in rows):
+            raise ValueError("mats: (offset, rows, cols) or (offset, rows, cols, row stride) of each matrix")
+        if any(not -2 ** 31 <= v < 2 ** 31 for m in rows for v in m[1:3]):
+            raise ValueError("mats: rows and columns are 32-bit numbers")
+        arr = (ds_matrix_t * max(1, len(rows)))(*[ds_matrix_t(m[0], m[3] if len(m) == 4 else m[2], m[1], m[2]) for m in rows])
+        cfg = ds_ortho_config_t()
+        cfg.d, cfg.mats, cfg.n_mats, cfg.steps = int(d), arr, len(rows), int(steps)
+        cfg.eps, cfg.factor = float(eps), _FACTOR[scale] if isinstance(scale, str) else int(scale)
+        cfg.flags = (ORTHO_NESTEROV if nesterov else 0) | (ORTHO_HALF if half else 0)
+        if coef is not None:
+            c = np.asarray(coef, dtype=np.float32)
+            if c.shape == (3,):
+                c = np.tile(c, (max(1, int(steps)), 1))
+            if c.shape != (int(steps), 3):
+                raise ValueError(f"coef: shape {c.shape}, expected (3,) or ({int(steps)}, 3)")
+            c = np.ascontiguousarray(c)
+            cfg.coef = c.ctypes.data_as(C.POINTER(C.c_float))
+        self._h = C.c_void_p()
+        self.d, self.steps = int(d), int(steps)
+        _check(L.ds_ortho_create(C.byref(cfg), C.byref(self._h)), "ds_ortho_create")
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            torch.cuda.synchronize(self.device)
+            load_library().ds_ortho_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def orthogonalize(self, src: torch.Tensor, dst: torch.Tensor, stream=None):
+        """dst <- O(src) for every matrix; fp32 or bf16 vectors of d elements, in place where dst is src."""
+        if self._h.value is None:
+            raise ValueError("the plan is closed")
+        for t, what in ((src, "src"), (dst, "dst")):
+            if isinstance(t, torch.Tensor) and t.dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError(f"{what}: dtype {t.dtype}")
+            _need(t, what, getattr(t, "dtype", None), (self.d,))
+        _one_device(self.device, src=src, dst=dst)
+        lo, hi = src.data_ptr(), src.data_ptr() + src.numel() * src.element_size()
+        if not (src.data_ptr() == dst.data_ptr() and src.dtype == dst.dtype) and \
+                dst.data_ptr() < hi and lo < dst.data_ptr() + dst.numel() * dst.element_size():
+            raise ValueError("dst: overlaps src without being it")
+        _check(load_library().ds_orthogonalize(self._h, src.data_ptr(), BF16 if src.dtype == torch.bfloat16 else F32, dst.data_ptr(),
+                                               BF16 if dst.dtype == torch.bfloat16 else F32, _stream_ptr(stream, self.device)),
+               "ds_orthogonalize")
 
 
 # -- the C names, as plain functions ------------------------------------------------------
@@ -413,6 +538,27 @@ def ds_server_aggregate_compress(ctx: Context, step, inp, delta_s, out, stream=N
 
 def ds_apply_update(ctx: Context, srv, x, m, gamma, beta=0.0, stream=None):
     ctx.apply_update(srv, x, m, gamma, beta, stream)
+
+
+def ds_ortho_create(*args, **kw) -> OrthoPlan:
+    return OrthoPlan(*args, **kw)
+
+
+def ds_ortho_destroy(plan: OrthoPlan) -> None:
+    plan.close()
+
+
+def ds_orthogonalize(plan: OrthoPlan, src, dst, stream=None):
+    plan.orthogonalize(src, dst, stream)
+
+
+def ds_apply_update_ortho(ctx: Context, plan: OrthoPlan, srv, x, m, gamma, beta=0.0, decay=0.0, stream=None):
+    ctx.apply_update_ortho(plan, srv, x, m, gamma, beta, decay, stream)
+
+
+def ds_apply_update_adamw(ctx: Context, srv, step, x, m, v, gamma, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.0, skip=None,
+                          stream=None):
+    ctx.apply_update_adamw(srv, step, x, m, v, gamma, beta1, beta2, eps, decay, skip, stream)
 
 
 def ds_decompress(ctx: Context, p, row, out, stream=None):

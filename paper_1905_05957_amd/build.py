@@ -11,8 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libds_hip.so")
 FASTCALL, FASTCALL_SRC = os.path.join(HERE, "_fastcall.so"), os.path.join(CSRC, "fastcall.cpp")
-SOURCES = ["ds_api.hip", "identity.hip", "sign.hip", "qsgd.hip", "topk.hip", "clip.hip", "rsparse.hip", "ternary.hip"]
-HEADERS = ["ds_device.h", "held.h", "ds_internal.h", os.path.join("..", "..", "include", "ds.h")]
+SOURCES = ["ds_api.hip", "identity.hip", "sign.hip", "qsgd.hip", "topk.hip", "clip.hip", "rsparse.hip", "ternary.hip", "ortho.hip"]
+HEADERS = ["ds_device.h", "held.h", "ds_internal.h", "tails.h", os.path.join("..", "..", "include", "ds.h")]
 
 # -ffp-contract=off: every fused multiply-add in the kernels is an explicit __fmaf_rn, so
 #   results do not depend on the compiler's contraction choices.

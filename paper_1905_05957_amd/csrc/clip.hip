@@ -9,6 +9,7 @@
 // thread.
 #include "ds_device.h"
 #include "ds_internal.h"
+#include "tails.h"
 
 #include <type_traits>
 
@@ -211,6 +212,15 @@ __global__ __launch_bounds__(kBlock) void k_clip_update(const uint8_t *msg, floa
     apply_q4<MOM, DECODE_ONLY>(load_msg4<NB>(msg, e, d), e, d, x, m, gamma, beta);
 }
 
+template <int NB, class Tail>
+__global__ __launch_bounds__(kBlock) void k_clip_each(const uint8_t *msg, int64_t d, Tail tail)
+{
+    const int64_t e = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    if (e >= d) return;
+    const uint32_t f = tail.wants(e, d);
+    if (f) tail.put(load_msg4<NB>(msg, e, d), e, d, f);
+}
+
 unsigned blocks4(int64_t d) { return static_cast<unsigned>((d + kBlock * 4 - 1) / (kBlock * 4)); }
 
 uint32_t clip_mask(int bits) { return ~static_cast<uint32_t>((1ull << bits) - 1ull); }
@@ -311,3 +321,14 @@ ds_status_t ds_clip_decode(ds_ctx *c, const ds_payload_t *p, int32_t row, float 
     });
     return ds_launch_status();
 }
+
+template <class Tail>
+ds_status_t ds_clip_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
+{
+    with_bytes(c->cfg.levels, [&](auto nb) {
+        k_clip_each<decltype(nb)::value><<<blocks4(c->cfg.d), kBlock, 0, st>>>(srv->levels, c->cfg.d, tail);
+    });
+    return ds_launch_status();
+}
+template ds_status_t ds_clip_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);
+template ds_status_t ds_clip_each(ds_ctx *, const ds_payload_t *, const TailAdamW &, hipStream_t);

@@ -1,6 +1,9 @@
 // C-ABI of libds_hip.so: argument validation and dispatch to the per-compressor kernels.
 // The three step calls are the three blocks of Algorithm 1 of the DoubleSqueeze paper.
 #include "ds_internal.h"
+#include "tails.h"
+
+#include <math.h>
 
 #include <new>
 
@@ -53,23 +56,6 @@ ds_status_t check_server_payload(const ds_ctx *c, const ds_payload_t *p, bool ne
     if (!p->dense) return need_dense ? DS_ERR_NULL : DS_OK;
     return misaligned(p->dense) ? DS_ERR_ALIGN : DS_OK;
 }
-
-// Binds the calling thread to the context's device for the duration of a call.
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev)
-    {
-        if (hipGetDevice(&prev) != hipSuccess) { ok = false; return; }
-        if (prev != dev && hipSetDevice(dev) != hipSuccess) ok = false;
-        dev_ = dev;
-    }
-    ~DeviceGuard()
-    {
-        if (ok && prev != dev_) (void)hipSetDevice(prev);
-    }
-    int dev_ = -1;
-};
 
 }  // namespace
 
@@ -392,6 +378,63 @@ ds_status_t ds_server_aggregate_compress_update(ds_ctx_t *c, uint64_t step, cons
     rc = ds_server_aggregate_compress(c, step, in, delta_s, out, hip_stream);
     if (rc != DS_OK) return rc;
     return ds_apply_update(c, out, x, m, gamma, beta, hip_stream);
+}
+
+// One pass over the server's message that hands every decoded element to `tail`.
+extern "C++" {
+template <class Tail>
+static ds_status_t each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
+{
+    if (c->sid) return ds_identity_each(c, srv, tail, st);                  // the message is the dense average
+    switch (c->cfg.comp) {
+    case DS_COMP_IDENTITY: return ds_identity_each(c, srv, tail, st);
+    case DS_COMP_SIGN: return ds_sign_each(c, srv, tail, st);
+    case DS_COMP_TOPK: return ds_topk_each(c, srv, tail, st);
+    case DS_COMP_QSGD: return ds_qsgd_each(c, srv, tail, st);
+    case DS_COMP_CLIP: return ds_clip_each(c, srv, tail, st);
+    case DS_COMP_RSPARSE: return ds_rsparse_each(c, srv, tail, st);
+    case DS_COMP_TERNARY: return DS_ERR_UNSUPPORTED;                        // built with the uncompressed server only
+    }
+    return DS_ERR_CONFIG;
+}
+}
+
+ds_status_t ds_apply_update_ortho(ds_ctx_t *c, ds_ortho_t *plan, const ds_payload_t *srv, float *x, float *m, float gamma, float beta,
+                                  float decay, void *hip_stream)
+{
+    if (!c || !plan || !x) return DS_ERR_NULL;
+    const ds_status_t rc = check_server_payload(c, srv);
+    if (rc != DS_OK) return rc;
+    if (ds_ortho_elements(plan) != c->cfg.d) return DS_ERR_SHAPE;
+    if (ds_ortho_device(plan) != c->device) return DS_ERR_CONFIG;
+    if (misaligned(x) || (m && misaligned(m))) return DS_ERR_ALIGN;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return DS_ERR_DEVICE;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    float *u = !m || ds_ortho_nesterov(plan) ? ds_ortho_buffer(plan) : nullptr;
+    const ds_status_t done = each(c, srv, ds::TailMomentum{ds_ortho_inside(plan), m, u, beta}, st);
+    if (done != DS_OK) return done;
+    return ds_ortho_update(plan, u ? u : m, x, gamma, decay, st);
+}
+
+ds_status_t ds_apply_update_adamw(ds_ctx_t *c, const ds_ortho_t *skip, const ds_payload_t *srv, uint64_t step, float *x, float *m,
+                                  float *v, double gamma, double beta1, double beta2, double eps, double decay, void *hip_stream)
+{
+    if (!c || !x || !m || !v) return DS_ERR_NULL;
+    const ds_status_t rc = check_server_payload(c, srv);
+    if (rc != DS_OK) return rc;
+    if (skip && ds_ortho_elements(skip) != c->cfg.d) return DS_ERR_SHAPE;
+    if (skip && ds_ortho_device(skip) != c->device) return DS_ERR_CONFIG;
+    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0 && eps >= 0.0)) return DS_ERR_CONFIG;
+    if (misaligned(x) || misaligned(m) || misaligned(v)) return DS_ERR_ALIGN;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return DS_ERR_DEVICE;
+    const double t = static_cast<double>(step) + 1.0;
+    const ds::TailAdamW tail{skip ? ds_ortho_inside(skip) : nullptr, x, m, v, static_cast<float>(beta1),
+                             static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
+                             static_cast<float>(gamma / (1.0 - pow(beta1, t))), static_cast<float>(1.0 / sqrt(1.0 - pow(beta2, t))),
+                             static_cast<float>(eps), static_cast<float>(1.0 - gamma * decay)};
+    return each(c, srv, tail, static_cast<hipStream_t>(hip_stream));
 }
 
 ds_status_t ds_materialize_error(ds_ctx_t *c, float *delta, int64_t delta_row_stride, float *delta_s, void *hip_stream)

@@ -96,6 +96,23 @@ static inline bool ds_stream_worthwhile(int64_t d)
     return d * 4 > (static_cast<int64_t>(64) << 20);
 }
 
+// Binds the calling thread to a context's or a plan's device for the duration of a call.
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = true;
+    explicit DeviceGuard(int dev)
+    {
+        if (hipGetDevice(&prev) != hipSuccess) { ok = false; return; }
+        if (prev != dev && hipSetDevice(dev) != hipSuccess) ok = false;
+        dev_ = dev;
+    }
+    ~DeviceGuard()
+    {
+        if (ok && prev != dev_) (void)hipSetDevice(prev);
+    }
+    int dev_ = -1;
+};
+
 // identity.hip
 ds_status_t ds_identity_worker(ds_ctx *c, const void *g, int64_t gs, float *delta, int64_t dstr,
                                const ds_payload_t *out, hipStream_t st);
@@ -179,3 +196,20 @@ ds_status_t ds_topk_server(ds_ctx *c, const ds_payload_t *in, float *delta_s,
 ds_status_t ds_topk_update(ds_ctx *c, const ds_payload_t *srv, float *x, float *m, float gamma,
                            float beta, hipStream_t st);
 ds_status_t ds_topk_decode(ds_ctx *c, const ds_payload_t *p, int32_t row, float *out, hipStream_t st);
+
+// The server's message decoded in one pass whose elements go to a tail (tails.h: TailMomentum, TailAdamW), per compressor.
+template <class Tail> ds_status_t ds_identity_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st);
+template <class Tail> ds_status_t ds_sign_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st);
+template <class Tail> ds_status_t ds_topk_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st);
+template <class Tail> ds_status_t ds_qsgd_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st);
+template <class Tail> ds_status_t ds_clip_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st);
+template <class Tail> ds_status_t ds_rsparse_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st);
+
+// ortho.hip: what the update calls need of a plan, and the matrices of `u` orthogonalised into the model
+// (x <- (1 - gamma * decay) x - gamma O(u)).
+const uint64_t *ds_ortho_inside(const ds_ortho *o);      // plane of bits: the elements of its matrices
+int64_t ds_ortho_elements(const ds_ortho *o);
+int ds_ortho_device(const ds_ortho *o);
+bool ds_ortho_nesterov(const ds_ortho *o);
+float *ds_ortho_buffer(const ds_ortho *o);               // [d]
+ds_status_t ds_ortho_update(const ds_ortho *o, const float *u, float *x, float gamma, float decay, hipStream_t st);

@@ -3,6 +3,7 @@
 // test mode that ties the three calls to a textbook routine.
 #include "ds_device.h"
 #include "ds_internal.h"
+#include "tails.h"
 
 using namespace ds;
 
@@ -64,6 +65,15 @@ __global__ __launch_bounds__(kBlock) void k_identity_update(const float *q_in, f
     }
 }
 
+template <class Tail>
+__global__ __launch_bounds__(kBlock) void k_identity_each(const float *q_in, int64_t d, Tail tail)
+{
+    const int64_t e = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    if (e >= d) return;
+    const uint32_t f = tail.wants(e, d);
+    if (f) tail.put(ld4_stream(q_in, e, d), e, d, f);
+}
+
 unsigned blocks4(int64_t d) { return static_cast<unsigned>((d + kBlock * 4 - 1) / (kBlock * 4)); }
 
 // Measurement aid: a plain copy in the shape of the library's dense passes (512 threads, one
@@ -122,3 +132,12 @@ ds_status_t ds_identity_decode(ds_ctx *c, const ds_payload_t *p, int32_t row, fl
                                                                         c->cfg.d, 0.f, 0.f);
     return ds_launch_status();
 }
+
+template <class Tail>
+ds_status_t ds_identity_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
+{
+    k_identity_each<<<blocks4(c->cfg.d), kBlock, 0, st>>>(srv->dense, c->cfg.d, tail);
+    return ds_launch_status();
+}
+template ds_status_t ds_identity_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);
+template ds_status_t ds_identity_each(ds_ctx *, const ds_payload_t *, const TailAdamW &, hipStream_t);

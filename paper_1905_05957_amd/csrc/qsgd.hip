@@ -16,6 +16,7 @@
 // sign bits and delta' = v - Q[v] all from registers.
 #include "ds_device.h"
 #include "ds_internal.h"
+#include "tails.h"
 
 #include <type_traits>
 
@@ -330,6 +331,18 @@ __global__ __launch_bounds__(kBlock) void k_qsgd_update(const uint8_t *levels, c
     apply_q4<MOM, DECODE_ONLY>(zero_past(q, e, P.d), e, P.d, x, m, gamma, beta);
 }
 
+template <class Tail>
+__global__ __launch_bounds__(kBlock) void k_qsgd_each(const uint8_t *levels, const uint64_t *words, const float *norms, QParams P,
+                                                      Tail tail)
+{
+    const int64_t e = static_cast<int64_t>(blockIdx.x) * kTile + threadIdx.x * 4;
+    if (e >= P.d) return;
+    const uint32_t f = tail.wants(e, P.d);
+    if (!f) return;
+    const float unit = __fdiv_rn(norms[e >> P.bshift], static_cast<float>(P.s));
+    tail.put(decode4(load_codes4(levels, e, P.d), load_sign_nibble(words, e), unit), e, P.d, f);
+}
+
 bool bucket_ok(int32_t b) { return b >= 64 && b <= kTile && (b & (b - 1)) == 0; }
 
 QParams make_params(const ds_ctx *c, uint64_t step)
@@ -438,3 +451,14 @@ ds_status_t ds_qsgd_decode(ds_ctx *c, const ds_payload_t *p, int32_t row, float 
         p->levels + row * ((P.d + 1) / 2), p->sign_words + row * P.W, p->scales + row * P.Bq, P, out, nullptr, 0.f, 0.f);
     return ds_launch_status();
 }
+
+template <class Tail>
+ds_status_t ds_qsgd_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
+{
+    if (!bucket_ok(c->cfg.bucket)) return DS_ERR_UNSUPPORTED;
+    k_qsgd_each<<<static_cast<unsigned>(c->n_tiles), kBlock, 0, st>>>(srv->levels, srv->sign_words, srv->scales, make_params(c, 0),
+                                                                      tail);
+    return ds_launch_status();
+}
+template ds_status_t ds_qsgd_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);
+template ds_status_t ds_qsgd_each(ds_ctx *, const ds_payload_t *, const TailAdamW &, hipStream_t);

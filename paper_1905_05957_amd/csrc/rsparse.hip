@@ -27,6 +27,7 @@
 // next) took 120 us more, not 75 us less: the pass needs every wavefront slot for its loads in flight.
 #include "ds_device.h"
 #include "ds_internal.h"
+#include "tails.h"
 
 #include <new>
 
@@ -415,6 +416,28 @@ __global__ __launch_bounds__(kBlock) void k_rs_apply(const uint64_t *__restrict_
     }
 }
 
+template <class Tail>
+__global__ __launch_bounds__(kBlock) void k_rs_each(const uint64_t *__restrict__ words, const float *__restrict__ vals,
+                                                    const uint32_t *__restrict__ off, int64_t d, int64_t n_sub, Tail tail)
+{
+    const int64_t e = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    const int64_t sub = e >> 8;
+    if (sub >= n_sub) return;                               // whole wavefronts
+    const uint32_t nib = (e < d) ? (load_sign_nibble(words, e) & valid_nibble(e, d)) : 0u;
+    const Ranks rk = subtile_ranks(nib);
+    if (e >= d) return;
+    const uint32_t f = tail.wants(e, d);
+    if (!f) return;
+    const float *src = vals + off[sub] + rk.before;
+    f32x4 q = {0.f, 0.f, 0.f, 0.f};
+    uint32_t r = 0;
+    if (nib & 1u) q.x = src[r++];
+    if (nib & 2u) q.y = src[r++];
+    if (nib & 4u) q.z = src[r++];
+    if (nib & 8u) q.w = src[r++];
+    tail.put(q, e, d, f);
+}
+
 unsigned blocks4(int64_t d) { return static_cast<unsigned>((d + kBlock * 4 - 1) / (kBlock * 4)); }
 
 
@@ -525,18 +548,23 @@ ds_status_t ds_rsparse_server(ds_ctx *c, uint64_t step, const ds_payload_t *in, 
 // p < 1/16: most 64-byte lines of x hold no kept element, and a plain update touches only those that do
 static bool sparse_update(const ds_ctx *c, const float *m) { return !m && c->cfg.k < (1 << 20); }
 
+// Offsets of the packed values of a message from its own plane.
+static const uint32_t *rs_offsets(ds_ctx *c, const uint64_t *words, hipStream_t st)
+{
+    ds_rs_scratch *t = c->rs;
+    k_rs_popcounts<<<static_cast<unsigned>((t->n_sub + kBlock - 1) / kBlock), kBlock, 0, st>>>(words, t->off_r, t->tot64, t->n_sub,
+                                                                                             t->n_t64, c->cfg.d);
+    scan_rows(t, t->off_r, 1, st);
+    return t->off_r;
+}
+
 // off == nullptr: the offsets of the packed values are derived from the message's own plane.
 template <bool DECODE_ONLY>
 static ds_status_t rs_apply(ds_ctx *c, const uint64_t *words, const float *vals, float *x, float *m, float gamma, float beta,
                             hipStream_t st, const uint32_t *off = nullptr)
 {
     ds_rs_scratch *t = c->rs;
-    if (!off) {
-        k_rs_popcounts<<<static_cast<unsigned>((t->n_sub + kBlock - 1) / kBlock), kBlock, 0, st>>>(
-            words, t->off_r, t->tot64, t->n_sub, t->n_t64, c->cfg.d);
-        scan_rows(t, t->off_r, 1, st);
-        off = t->off_r;
-    }
+    if (!off) off = rs_offsets(c, words, st);
     const unsigned blocks = blocks4(t->n_sub * kSub);
     if (DECODE_ONLY)
         k_rs_apply<false, true, false><<<blocks, kBlock, 0, st>>>(words, vals, off, x, nullptr, c->cfg.d, c->W, t->n_sub, 0.f, 0.f);
@@ -571,3 +599,13 @@ ds_status_t ds_rsparse_decode(ds_ctx *c, const ds_payload_t *p, int32_t row, flo
     return rs_apply<true>(c, p->sign_words + static_cast<int64_t>(row) * c->W, p->dense + static_cast<int64_t>(row) * c->cfg.d,
                           out, nullptr, 0.f, 0.f, st);
 }
+
+template <class Tail>
+ds_status_t ds_rsparse_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
+{
+    const uint32_t *off = rs_offsets(c, srv->sign_words, st);
+    k_rs_each<<<blocks4(c->rs->n_sub * kSub), kBlock, 0, st>>>(srv->sign_words, srv->dense, off, c->cfg.d, c->rs->n_sub, tail);
+    return ds_launch_status();
+}
+template ds_status_t ds_rsparse_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);
+template ds_status_t ds_rsparse_each(ds_ctx *, const ds_payload_t *, const TailAdamW &, hipStream_t);

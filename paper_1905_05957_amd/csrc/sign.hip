@@ -19,6 +19,7 @@
 // the shape, so results are bit-reproducible run to run.
 #include "ds_device.h"
 #include "ds_internal.h"
+#include "tails.h"
 #include "held.h"
 
 #include <mutex>
@@ -288,6 +289,19 @@ __global__ __launch_bounds__(kBlock) void k_sign_chunk_update(const uint64_t *__
     const float s = scales[static_cast<uint32_t>(e) / static_cast<uint32_t>(chunk)];
     const uint32_t nib = load_sign_nibble(words, e);
     apply_q4<MOM, DECODE_ONLY>(signed4(s, s, s, s, nib), e, d, x, m, gamma, beta);
+}
+
+// The same for a pass with a tail of its own.
+template <class Tail>
+__global__ __launch_bounds__(kBlock) void k_sign_chunk_each(const uint64_t *__restrict__ words, const float *__restrict__ scales,
+                                                            int64_t chunk, int64_t d, Tail tail)
+{
+    const int64_t e = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    if (e >= d) return;
+    const uint32_t f = tail.wants(e, d);
+    if (!f) return;
+    const float s = scales[static_cast<uint32_t>(e) / static_cast<uint32_t>(chunk)];
+    tail.put(signed4(s, s, s, s, load_sign_nibble(words, e)), e, d, f);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1041,6 +1055,23 @@ __global__ __launch_bounds__(kBlock) void k_sign_update(const uint64_t *__restri
     }
 }
 
+template <class Tail>
+__global__ __launch_bounds__(kBlock) void k_sign_each(const uint64_t *__restrict__ words, const float *__restrict__ scales,
+                                                      ds_sign_tables tb, int64_t d, Tail tail)
+{
+    const int64_t tile = blockIdx.x;
+    const int64_t e = tile * kTile + threadIdx.x * 4;
+    if (e >= d) return;
+    const uint32_t f = tail.wants(e, d);
+    if (!f) return;
+    const TilePieces tp = tile_pieces(tb, tile);
+    float s[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        s[c] = (e + c < d) ? scales[tp.seg0 >= 0 ? tp.seg0 : seg_of(tb, tp.p0, tp.p1, e + c)] : 0.f;
+    tail.put(signed4(s[0], s[1], s[2], s[3], load_sign_nibble(words, e)), e, d, f);
+}
+
 // Server that does not compress (Section 5.1 "MEM-SGD"): a = (1/n) sum_i Q[v_i] by the chain
 // from +0, per element: the element's bit and the scale of its group from every worker's
 // message.  CHUNKS: the groups are chunks of `chunk` elements (a multiple of 4), else they come
@@ -1510,3 +1541,14 @@ extern "C" ds_status_t ds_worker_compress_sign_noalloc(int32_t n, int64_t d, int
     sign_pass2(delta, delta_row_stride, d, n, scales, 1, tb, st);
     return ds_launch_status();
 }
+
+template <class Tail>
+ds_status_t ds_sign_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
+{
+    const unsigned blocks = static_cast<unsigned>(c->n_tiles);
+    if (c->sign_fused) k_sign_chunk_each<<<blocks, kBlock, 0, st>>>(srv->sign_words, srv->scales, c->cfg.chunk, c->cfg.d, tail);
+    else k_sign_each<<<blocks, kBlock, 0, st>>>(srv->sign_words, srv->scales, c->sign_tb, c->cfg.d, tail);
+    return ds_launch_status();
+}
+template ds_status_t ds_sign_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);
+template ds_status_t ds_sign_each(ds_ctx *, const ds_payload_t *, const TailAdamW &, hipStream_t);

@@ -35,6 +35,7 @@
 // bit-reproducible and the two routes agree bit for bit.
 #include "ds_device.h"
 #include "ds_internal.h"
+#include "tails.h"
 #include "held.h"
 
 #include <new>
@@ -2160,6 +2161,28 @@ __global__ __launch_bounds__(kBlock) void k_topk_dense_apply(const u32x2 *pairs,
     apply_q4<MOM, DECODE_ONLY>(q, e, d, x, m, gamma, beta);
 }
 
+template <class Tail>
+__global__ __launch_bounds__(kBlock) void k_topk_each(const u32x2 *pairs, int64_t k, int64_t d, Tail tail)
+{
+    __shared__ __attribute__((aligned(16))) float tilev[kTile];
+    __shared__ int64_t range[2];
+    const int64_t base = static_cast<int64_t>(blockIdx.x) * kTile;
+    const int64_t e = base + threadIdx.x * 4;
+    const uint32_t f = (e < d) ? tail.wants(e, d) : 0u;
+    if (!__syncthreads_or(static_cast<int>(f))) return;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) tilev[threadIdx.x * 4 + c] = 0.f;
+    if (threadIdx.x < 2) range[threadIdx.x] = lower_bound_idx(pairs, k, base + threadIdx.x * kTile);
+    __syncthreads();
+    for (int64_t j = range[0] + threadIdx.x; j < range[1]; j += kBlock) {
+        const u32x2 pr = pairs[j];
+        const uint32_t rel = pr.x - static_cast<uint32_t>(base);
+        if (rel < static_cast<uint32_t>(kTile)) tilev[rel] = __uint_as_float(pr.y);
+    }
+    __syncthreads();
+    if (f) tail.put(*reinterpret_cast<const f32x4 *>(&tilev[threadIdx.x * 4]), e, d, f);
+}
+
 // Zeroes up to five arrays of 32-bit words (the context's scratch state after a failed launch).
 __global__ __launch_bounds__(kBlock) void k_topk_clear(uint32_t *a, int64_t na, uint32_t *b, int64_t nb, uint32_t *c,
                                                        int64_t nc, uint32_t *d, int64_t nd, uint32_t *e, int64_t ne)
@@ -2465,3 +2488,13 @@ ds_status_t ds_topk_decode(ds_ctx *c, const ds_payload_t *p, int32_t row, float 
                                                                                        c->cfg.d, 0.f, 0.f);
     return ds_launch_status();
 }
+
+template <class Tail>
+ds_status_t ds_topk_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
+{
+    k_topk_each<<<static_cast<unsigned>(c->n_tiles), kBlock, 0, st>>>(reinterpret_cast<const u32x2 *>(srv->pairs), c->cfg.k, c->cfg.d,
+                                                                     tail);
+    return ds_launch_status();
+}
+template ds_status_t ds_topk_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);
+template ds_status_t ds_topk_each(ds_ctx *, const ds_payload_t *, const TailAdamW &, hipStream_t);

@@ -1,0 +1,400 @@
+"""GPU: orthogonalisation by Newton-Schulz products and the model update through it, against the same iteration in 64 bits.
+
+Tolerance.  What is stored between products is rounded relative to its value by u = 2^-22 (two halves of 11 bits) or 2^-11
+(one).  Relative to ||X|| a step adds u for X, |b| + 2 |c| < 9 times u for G = X X' (its norm is at most 1.4) and
+about 3 u for B: 16 u; sums over K terms in fp32 add at most 4 sqrt(K) 2^-24 of their value (errors of either sign).
+That is carried through `steps` steps; the iteration itself does not enlarge errors relative to X for inputs whose singular
+values are of one size, as those of the random matrices here are.  Errors of single elements: six times the root
+mean square that the norm's bound stands for.  Then the rounding to the output's type."""
+import math
+
+import pytest
+import torch
+
+import paper_1905_05957_amd as P
+
+pytestmark = pytest.mark.gpu
+COEF = (3.4445, -4.7750, 2.0315)
+
+
+def reference(u, steps=5, coef=COEF, eps=1e-7, scale="none"):
+    """O(u) in 64 bits."""
+    r, c = u.shape
+    x = u.double()
+    norm = x.square().sum().sqrt() + eps
+    x = x / norm if norm > 0 else x
+    x = x.t().contiguous() if r > c else x
+    table = [coef] * steps if not isinstance(coef[0], (list, tuple)) else coef
+    for a, b, k in table:
+        g = x @ x.t()
+        x = a * x + (b * g + k * (g @ g)) @ x
+    x = x.t() if r > c else x
+    return x * {"none": 1.0, "aspect": math.sqrt(max(1.0, r / c)), "rms": 0.2 * math.sqrt(max(r, c))}[scale]
+
+
+def bound(shape, half, steps=5):
+    u = 2.0 ** -11 if half else 2.0 ** -22
+    return steps * (16 * u + 4 * math.sqrt(max(shape)) * 2.0 ** -24)
+
+
+def check(got, want, half, steps=5, extra=0.0):
+    """got of any type against want in 64 bits."""
+    rounding = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}[got.dtype]
+    tol = bound(want.shape, half, steps) + extra
+    err = (got.double() - want).abs()
+    rms = want.square().mean().sqrt()
+    assert torch.isfinite(got).all()
+    assert err.square().mean().sqrt() <= (tol + rounding) * rms, (want.shape, float(err.square().mean().sqrt() / rms), tol)
+    assert (err <= 6 * tol * rms + rounding * want.abs() * 1.01).all(), (want.shape, float(err.max() / rms), tol)
+
+
+def view(flat, mat):
+    offset, r, c = mat[:3]
+    return flat.as_strided((r, c), (mat[3] if len(mat) > 3 else c, 1), flat.storage_offset() + offset)
+
+
+def random_flat(d, dev, seed, dtype=torch.float32):
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(seed)
+    return torch.randn(d, generator=gen, device=dev).to(dtype)
+
+
+SHAPES = [(1, 1), (1, 2), (2, 1), (3, 3), (1, 64), (7, 1), (1, 513), (5, 33), (31, 32), (33, 31), (64, 64), (63, 65), (96, 64),
+          (64, 97), (128, 128), (129, 257), (127, 900), (255, 256), (257, 129), (333, 1001), (1000, 77), (640, 641), (513, 512)]
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"{s[0]}x{s[1]}")
+def test_one_matrix(gpu_device, shape, half):
+    r, c = shape
+    src = random_flat(r * c, gpu_device, 1)
+    plan = P.OrthoPlan(r * c, [(0, r, c)], half=half)
+    dst = torch.full_like(src, 7.0)
+    plan.orthogonalize(src, dst)
+    check(dst.view(r, c), reference(src.view(r, c)), half)
+    plan.close()
+
+
+@pytest.mark.parametrize("src_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dst_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("half", [False, True])
+def test_types(gpu_device, src_dtype, dst_dtype, half):
+    mats = [(3, 130, 70), (3 + 9100 + 5, 70, 130)]
+    src = random_flat(18300, gpu_device, 2, src_dtype)
+    plan = P.OrthoPlan(18300, mats, half=half)
+    dst = torch.zeros(18300, dtype=dst_dtype, device=gpu_device)
+    plan.orthogonalize(src, dst)
+    for m in mats:
+        check(view(dst, m), reference(view(src, m)), half)
+    if src_dtype == dst_dtype:                            # in place
+        plan.orthogonalize(src, src)
+        assert torch.equal(torch.cat([view(src, m).reshape(-1) for m in mats]), torch.cat([view(dst, m).reshape(-1) for m in mats]))
+    plan.close()
+
+
+def test_many_matrices_offsets_strides_and_what_lies_between(gpu_device):
+    """Odd offsets, column blocks of one array, a vector: elements between the matrices are neither read nor written."""
+    mats, at = [], 1
+    for r, c, parts in ((333, 101, 1), (96, 480, 3), (1, 700, 1), (200, 1, 1), (64, 65, 5), (300, 260, 1), (17, 17, 1)):
+        for p in range(parts):
+            mats.append((at + p * (c // parts), r, c // parts, c))
+        at += r * c + 7
+    d = at + 50
+    inside = torch.zeros(d, dtype=torch.bool, device=gpu_device)
+    for m in mats:
+        view(inside, m).fill_(True)
+    src = random_flat(d, gpu_device, 3)
+    src[~inside] = float("nan")
+    dst = torch.full((d,), 3.25, device=gpu_device)
+    plan = P.OrthoPlan(d, mats, scale="rms")
+    plan.orthogonalize(src, dst)
+    for m in mats:
+        check(view(dst, m), reference(view(src, m), scale="rms"), False)
+    assert (dst[~inside] == 3.25).all()
+    again = torch.zeros_like(dst)
+    plan.orthogonalize(src, again)
+    assert torch.equal(again[inside], dst[inside])        # the same bits every time
+    plan.close()
+
+
+@pytest.mark.parametrize("scale", ["none", "aspect", "rms"])
+@pytest.mark.parametrize("shape", [(150, 40), (40, 150), (70, 70)])
+def test_factors(gpu_device, scale, shape):
+    src = random_flat(shape[0] * shape[1], gpu_device, 4)
+    plan = P.OrthoPlan(src.numel(), [(0, *shape)], scale=scale)
+    dst = torch.empty_like(src)
+    plan.orthogonalize(src, dst)
+    check(dst.view(shape), reference(src.view(shape), scale=scale), False)
+    plan.close()
+
+
+@pytest.mark.parametrize("coef,steps", [(None, 1), (None, 7), ((1.5, -0.5, 0.0), 12),
+                                        ([(4.0, -6.5, 2.9), (3.9, -6.2, 2.8), (2.0, -1.5, 0.5)], 3)])
+def test_own_coefficients(gpu_device, coef, steps):
+    """Another list has another bound: each |b| and |c| of these is at most 1.4 times the standard's, hence 1.4 times 16 u."""
+    src = random_flat(90 * 200, gpu_device, 5)
+    plan = P.OrthoPlan(src.numel(), [(0, 90, 200)], steps=steps, coef=coef)
+    dst = torch.empty_like(src)
+    plan.orthogonalize(src, dst)
+    check(dst.view(90, 200), reference(src.view(90, 200), steps, coef or COEF), False, steps, extra=0.4 * bound((90, 200), False, steps))
+    plan.close()
+
+
+@pytest.mark.parametrize("half", [False, True])
+def test_matrices_of_zeros(gpu_device, half):
+    for eps in (0.0, 1e-7):
+        plan = P.OrthoPlan(3 * 6400, [(0, 80, 80), (6400, 80, 80), (12800, 80, 80)], eps=eps, half=half)
+        src = random_flat(3 * 6400, gpu_device, 6)
+        src[6400:12800] = 0.0
+        dst = torch.full_like(src, 5.0)
+        plan.orthogonalize(src, dst)
+        assert (dst[6400:12800] == 0.0).all()
+        for k in (0, 2):
+            check(dst[k * 6400:(k + 1) * 6400].view(80, 80), reference(src[k * 6400:(k + 1) * 6400].view(80, 80)), half)
+        plan.close()
+
+
+@pytest.mark.parametrize("size", [1e-36, 1e-30, 1e30, 3e37])
+def test_any_size_of_input(gpu_device, size):
+    """The norm is summed in 64 bits, so nothing overflows or vanishes; subnormal inputs (1e-36: some) are exact too."""
+    src = random_flat(100 * 60, gpu_device, 7) * size
+    plan = P.OrthoPlan(src.numel(), [(0, 100, 60)], eps=0.0)
+    dst = torch.empty_like(src)
+    plan.orthogonalize(src, dst)
+    check(dst.view(100, 60), reference(src.view(100, 60), eps=0.0), False)
+    plan.close()
+
+
+def test_eps_counts_for_small_inputs(gpu_device):
+    src = random_flat(100 * 60, gpu_device, 8) * 1e-9
+    plan = P.OrthoPlan(src.numel(), [(0, 100, 60)], eps=1e-7)
+    dst = torch.empty_like(src)
+    plan.orthogonalize(src, dst)
+    check(dst.view(100, 60), reference(src.view(100, 60), eps=1e-7), False)
+    plan.close()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_is_not_finite_stays_in_its_matrix(gpu_device, bad):
+    mats = [(0, 70, 90), (6300, 90, 70), (12600, 33, 65)]
+    src = random_flat(12600 + 33 * 65, gpu_device, 9)
+    src[6300 + 1234] = bad
+    dst = torch.zeros_like(src)
+    plan = P.OrthoPlan(src.numel(), mats)
+    plan.orthogonalize(src, dst)
+    assert torch.isnan(view(dst, mats[1])).any()
+    for m in (mats[0], mats[2]):
+        check(view(dst, m), reference(view(src, m)), False)
+    plan.close()
+
+
+def test_low_rank_and_one_large_entry(gpu_device):
+    """Rounding errors of X lie in all directions and grow 3.9 times a step at most (the polynomial's slope on [0, 1.2]), while the
+    bound of the other tests takes X to grow with them: 3.9^5 = 903 times the first step's 16 u ||X|| and less for
+    the others, and ||X|| = 1 at the start against at least 0.68 at the end."""
+    gen = torch.Generator(device=gpu_device)
+    gen.manual_seed(10)
+    low = torch.randn(150, 2, generator=gen, device=gpu_device) @ torch.randn(2, 400, generator=gen, device=gpu_device)
+    spike = torch.zeros(150, 400, device=gpu_device)
+    spike[17, 311] = -3.0
+    src = torch.cat([low.reshape(-1), spike.reshape(-1)])
+    plan = P.OrthoPlan(src.numel(), [(0, 150, 400), (60000, 150, 400)])
+    dst = torch.empty_like(src)
+    plan.orthogonalize(src, dst)
+    for k in range(2):
+        want = reference(src[k * 60000:(k + 1) * 60000].view(150, 400))
+        err = (dst[k * 60000:(k + 1) * 60000].view(150, 400).double() - want).norm()
+        assert err <= 2 * 903 * 16 * 2.0 ** -22 / 0.68 * want.norm()
+    plan.close()
+
+
+@pytest.mark.parametrize("shape,half", [((768, 2048), False), ((2048, 768), True), ((1024, 1024), False), ((2100, 1900), False),
+                                        ((1, 70000), False), ((20000, 40), True)])
+def test_large(gpu_device, shape, half):
+    src = random_flat(shape[0] * shape[1], gpu_device, 11)
+    plan = P.OrthoPlan(src.numel(), [(0, *shape)], half=half)
+    dst = torch.empty_like(src)
+    plan.orthogonalize(src, dst)
+    check(dst.view(shape), reference(src.view(shape)), half)
+    plan.close()
+
+
+# ---------------------------------------------------------------------------------------
+# the update
+# ---------------------------------------------------------------------------------------
+BOTH = P.FLAG_SERVER_IDENTITY | P.FLAG_NO_ERROR_FEEDBACK
+COMPRESSORS = [("identity", {}, 0), ("sign", dict(scale_mode="chunk", chunk=2048), 0), ("sign", dict(scale_mode="whole"), 0),
+               ("sign", dict(scale_mode="segments", seg_offsets=[0, 777, 9000, 20011, 50123]), 0),
+               ("sign", dict(scale_mode="chunk", chunk=100), 0), ("topk", dict(k=500), 0), ("qsgd", dict(bucket=512, levels=15), 0),
+               ("clip", dict(levels=16), 0), ("clip", dict(levels=24), 0), ("clip", dict(levels=8), 0), ("rsparse", dict(keep_prob=0.6), 0),
+               ("topk", dict(k=500), BOTH), ("sign", dict(scale_mode="whole"), P.FLAG_SERVER_IDENTITY), ("ternary", {}, BOTH)]
+MATS = [(5, 100, 130), (13010, 64, 64), (17106, 90, 33, 100), (17106 + 33, 90, 67, 100), (26108, 1, 301), (26500, 150, 150)]
+D = 50123
+
+
+def message(comp, kw, flags, dev, seed=20):
+    ctx = P.Context(comp, 2, D, flags=flags, **kw)
+    g = random_flat(2 * D, dev, seed).view(2, D) * 1e-2
+    delta = None if flags & P.FLAG_NO_ERROR_FEEDBACK else torch.zeros(2, D, device=dev)
+    delta_s = None if flags else torch.zeros(D, device=dev)
+    pw, ps = ctx.alloc_payload(2), ctx.alloc_server_payload()
+    ctx.worker_compress(0, g, delta, pw)
+    ctx.server_aggregate_compress(0, pw, delta_s, ps)
+    q = torch.empty(D, device=dev)
+    ctx.decompress(ps, 0, q)
+    return ctx, ps, q
+
+
+def state(dev, seed=30):
+    return random_flat(D, dev, seed) * 0.02, random_flat(D, dev, seed + 1) * 1e-2
+
+
+def expected(plan_kw, q, x, m, gamma, beta, decay, half=False):
+    """New x and m in 64 bits, and how far x may be off."""
+    x, m, off = x.double(), m.double() if m is not None else None, torch.zeros_like(x, dtype=torch.float64)
+    for mat in MATS:
+        u = view(q, mat).double()
+        if m is not None:
+            mm = view(m, mat)
+            mm.mul_(beta).add_(view(q, mat).double())
+            u = beta * mm + u if plan_kw.get("nesterov") else mm
+        o = reference(u, scale=plan_kw.get("scale", "none"))
+        xm, fm = view(x, mat), view(off, mat)
+        # the product with keep, the fma and keep itself: a rounding each; gamma in fp32 one more
+        fm.copy_(3 * 2.0 ** -24 * (xm.abs() + gamma * o.abs()) + 6 * gamma * bound(o.shape, half) * o.square().mean().sqrt())
+        xm.mul_(1.0 - gamma * decay).sub_(gamma * o)
+    return x, m, off
+
+
+@pytest.mark.parametrize("comp,kw,flags", COMPRESSORS, ids=lambda v: v if isinstance(v, str) else None)
+def test_update_from_every_message(gpu_device, comp, kw, flags):
+    ctx, ps, q = message(comp, kw, flags, gpu_device)
+    x, m = state(gpu_device)
+    gamma, beta, decay = 0.03125, 0.875, 0.25             # exact in fp32
+    kwp = dict(nesterov=True, scale="aspect")
+    want_x, want_m, off = expected(kwp, q, x, m, gamma, beta, decay)
+    before_x, before_m = x.clone(), m.clone()
+    plan = P.OrthoPlan(D, MATS, **kwp)
+    ctx.apply_update_ortho(plan, ps, x, m, gamma, beta, decay)
+    # one fma of exact operands
+    assert ((m.double() - want_m).abs() <= 2.0 ** -24 * want_m.abs() * 1.0001).all()
+    assert ((x.double() - want_x).abs() <= off).all(), float(((x.double() - want_x).abs() - off).max())
+    inside = torch.zeros(D, dtype=torch.bool, device=gpu_device)
+    for mat in MATS:
+        view(inside, mat).fill_(True)
+    assert torch.equal(x[~inside], before_x[~inside]) and torch.equal(m[~inside], before_m[~inside])
+    plan.close()
+    ctx.close()
+
+
+@pytest.mark.parametrize("nesterov,momentum,decay,half", [(False, True, 0.0, False), (True, True, 0.0, True), (False, False, 0.5, False),
+                                                          (True, False, 0.0, False)])
+def test_update_forms(gpu_device, nesterov, momentum, decay, half):
+    ctx, ps, q = message("qsgd", dict(bucket=128, levels=15), 0, gpu_device)
+    x, m = state(gpu_device)
+    m = m if momentum else None
+    kwp = dict(nesterov=nesterov, scale="rms")
+    want_x, want_m, off = expected(kwp, q, x, m, 0.0625, 0.9375, decay, half)
+    plan = P.OrthoPlan(D, MATS, half=half, **kwp)
+    ctx.apply_update_ortho(plan, ps, x, m, 0.0625, 0.9375, decay)
+    if momentum:
+        assert ((m.double() - want_m).abs() <= 2.0 ** -24 * want_m.abs() * 1.0001).all()
+    assert ((x.double() - want_x).abs() <= off).all()
+    plan.close()
+    ctx.close()
+
+
+def test_a_graph_replays_the_update(gpu_device):
+    """Worker, server, the update of the matrices and AdamW on the rest, captured, against the same calls made one by one."""
+    def make():
+        ctx = P.Context("sign", 2, D, scale_mode="chunk", chunk=2048)
+        plan = P.OrthoPlan(D, MATS, nesterov=True)
+        x, m = state(gpu_device)
+        v = torch.zeros(D, device=gpu_device)
+        g = random_flat(2 * D, gpu_device, 40).view(2, D) * 1e-2
+        delta, delta_s = torch.zeros(2, D, device=gpu_device), torch.zeros(D, device=gpu_device)
+        pw, ps = ctx.alloc_payload(2), ctx.alloc_payload(1)
+
+        def step():
+            ctx.worker_compress(0, g, delta, pw)
+            ctx.server_aggregate_compress(0, pw, delta_s, ps)
+            ctx.apply_update_ortho(plan, ps, x, m, 0.02, 0.9, 0.1)
+            ctx.apply_update_adamw(ps, 3, x, m, v, 1e-3, 0.9, 0.95, 1e-8, 0.1, skip=plan)
+        return step, (x, m, v, delta, delta_s), (ctx, plan, g, pw, ps)
+
+    eager, a, keep_a = make()
+    captured, b, keep_b = make()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        captured()
+    torch.cuda.current_stream().wait_stream(side)
+    eager()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured()
+    for _ in range(4):
+        graph.replay()
+        eager()
+        torch.cuda.synchronize()
+        for p, q in zip(a, b):
+            assert torch.equal(p, q)
+
+
+def test_streams_of_ones_own(gpu_device):
+    """Two plans on two streams at once, with nothing on the default stream to order them."""
+    srcs = [random_flat(300 * 500, gpu_device, 50 + k) for k in range(2)]
+    plans = [P.OrthoPlan(300 * 500, [(0, 300, 500)]) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    dsts = [torch.zeros(300 * 500, device=gpu_device) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for k in range(2):
+            plans[k].orthogonalize(srcs[k], dsts[k], stream=streams[k])
+    torch.cuda.synchronize()
+    for k in range(2):
+        check(dsts[k].view(300, 500), reference(srcs[k].view(300, 500)), False)
+        plans[k].close()
+
+
+def test_refusals_on_the_device(gpu_device):
+    from paper_1905_05957_amd import binding as B
+    dev = gpu_device
+    ctx, ps, _ = message("identity", {}, 0, dev)
+    plan, other = P.OrthoPlan(D, MATS), P.OrthoPlan(D - 1, [(0, 3, 3)])
+    x, m = state(dev)
+    before = x.clone(), m.clone()
+    closed = P.OrthoPlan(D, MATS)
+    closed.close()
+    wide = torch.zeros(2 * D + 8, device=dev)
+    bad = [
+        lambda: plan.orthogonalize(x.cpu(), x), lambda: plan.orthogonalize(x, m.double()), lambda: plan.orthogonalize(x[:-1], m),
+        lambda: plan.orthogonalize(x, wide[::2][:D]), lambda: closed.orthogonalize(x, m), lambda: plan.orthogonalize(x.half(), m),
+        lambda: plan.orthogonalize(wide[:D], wide[4:4 + D]), lambda: plan.orthogonalize(x, x.view(torch.bfloat16)[:D]),
+        lambda: plan.orthogonalize(None, x),
+        lambda: ctx.apply_update_ortho(other, ps, x, m, 0.1), lambda: ctx.apply_update_ortho(closed, ps, x, m, 0.1),
+        lambda: ctx.apply_update_ortho(None, ps, x, m, 0.1), lambda: ctx.apply_update_ortho(plan, ps, x[:-1], m, 0.1),
+        lambda: ctx.apply_update_ortho(plan, ps, x, m.double(), 0.1),
+        lambda: ctx.apply_update_adamw(ps, 0, x, m, None, 0.1), lambda: ctx.apply_update_adamw(ps, -1, x, m, m, 0.1),
+        lambda: ctx.apply_update_adamw(ps, 0, x, m, before[0], 0.1, skip=other),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} was taken")
+    with pytest.raises(P.DsError):
+        plan.orthogonalize(wide[1:1 + D], x)              # not 16-byte aligned
+    for kw in (dict(beta1=1.0), dict(beta2=-0.1), dict(beta1=float("nan")), dict(eps=-1e-8)):
+        with pytest.raises(P.DsError):
+            ctx.apply_update_adamw(ps, 0, x, m, before[1], 0.1, **kw)
+    L = P.load_library()
+    assert L.ds_orthogonalize(plan._h, x.data_ptr(), 0, m.data_ptr(), 2, None) == 3
+    assert L.ds_orthogonalize(plan._h, x.data_ptr(), 0, x.data_ptr(), 1, None) == 3
+    s = B.ds_payload_t()
+    import ctypes as C
+    assert L.ds_apply_update_ortho(ctx._h, plan._h, C.byref(s), x.data_ptr(), None, 0.1, 0.0, 0.0, None) == 1
+    assert L.ds_apply_update_ortho(ctx._h, other._h, C.byref(ps.c_struct()), x.data_ptr(), None, 0.1, 0.0, 0.0, None) == 2
+    torch.cuda.synchronize()
+    assert torch.equal(x, before[0]) and torch.equal(m, before[1])
+    for p in (plan, other, ctx):
+        p.close()
