@@ -14,8 +14,7 @@
 // With one half (DS_ORTHO_HALF) a rounding is 2^-11 at most; it grows with the smallest singular values at most, 3.44^5 = 485 times
 // while an entry of X grows as much or reaches 1 / sqrt(n), so it ends below a rounding to bf16.
 //
-// Layout.  All products have the form C[i][j] = sum_k P[i][k] Q[j][k] with k contiguous in both, so X is kept a second time
-// transposed.  A row is a sequence of 128-byte blocks: 32 values as 32 hi and 32 lo, or 64 values with one half.
+// Layout.  A row of an operand is a sequence of 128-byte blocks: 32 values as 32 hi and 32 lo, or 64 values with one half.
 #include "ds_device.h"
 #include "ds_internal.h"
 #include "tails.h"
@@ -31,7 +30,8 @@ using namespace ds;
 namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
@@ -44,7 +44,7 @@ constexpr int64_t kPartElements = 16384;
 
 struct Mat {
     int64_t offset, ld;          // in the vector
-    int64_t x, xt[2], g, b;      // byte offsets in the workspace
+    int64_t x[2], g, b;          // byte offsets in the workspace
     int32_t rows, cols;          // as stored
     int32_t m, n, mp, np;        // as worked on: m <= n, and rounded up to tiles
     int32_t row_n, row_m;        // bytes of a row of np and of mp values
@@ -60,7 +60,7 @@ struct Tile {
 };
 
 template <bool SPLIT>
-__device__ __forceinline__ int64_t chunk_at(int64_t row_bytes, int row, int k)     // k a multiple of 8
+__device__ __forceinline__ int64_t chunk_at(int64_t row_bytes, int row, int k)     // k a multiple of 4
 {
     return row * row_bytes + (SPLIT ? (k >> 5) * kRowBlock + (k & 31) * 2 : k * 2);
 }
@@ -79,15 +79,36 @@ __device__ __forceinline__ void store8(char *p, const float *v)
 }
 
 template <bool SPLIT>
-__device__ __forceinline__ void load8(const char *p, float *v)
+__device__ __forceinline__ void store4(char *p, const float *v)
 {
-    const half8 hi = *reinterpret_cast<const half8 *>(p);
+    half4 hi, lo;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = static_cast<float>(hi[t]);
+    for (int t = 0; t < 4; ++t) {
+        hi[t] = static_cast<_Float16>(v[t]);
+        lo[t] = static_cast<_Float16>(v[t] - static_cast<float>(hi[t]));
+    }
+    *reinterpret_cast<half4 *>(p) = hi;
+    if (SPLIT) *reinterpret_cast<half4 *>(p + kRowBlock / 2) = lo;
+}
+
+template <bool SPLIT>
+__device__ __forceinline__ void store1(char *p, float v)
+{
+    const _Float16 hi = static_cast<_Float16>(v);
+    *reinterpret_cast<_Float16 *>(p) = hi;
+    if (SPLIT) *reinterpret_cast<_Float16 *>(p + kRowBlock / 2) = static_cast<_Float16>(v - static_cast<float>(hi));
+}
+
+template <bool SPLIT>
+__device__ __forceinline__ void load4(const char *p, float *v)
+{
+    const half4 hi = *reinterpret_cast<const half4 *>(p);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = static_cast<float>(hi[t]);
     if (SPLIT) {
-        const half8 lo = *reinterpret_cast<const half8 *>(p + kRowBlock / 2);
+        const half4 lo = *reinterpret_cast<const half4 *>(p + kRowBlock / 2);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] += static_cast<float>(lo[t]);
+        for (int t = 0; t < 4; ++t) v[t] += static_cast<float>(lo[t]);
     }
 }
 
@@ -128,7 +149,7 @@ __global__ __launch_bounds__(kBlock) void k_ortho_norm(const Mat *__restrict__ m
     if (threadIdx.x == 0) partial[M.part0 + pt.y] = s;
 }
 
-// X = U / (norm + eps), times 2^s, both ways round, zero beyond the matrix.
+// X = U / (norm + eps), times 2^s, zero beyond the matrix.
 template <bool SPLIT, bool BF16>
 __global__ __launch_bounds__(kThreads) void k_ortho_operands(const Mat *__restrict__ mats, const Tile *__restrict__ tiles,
                                                              const void *src, const double *__restrict__ partial, float eps, char *ws)
@@ -165,10 +186,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_operands(const Mat *__restri
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = tile[a][c + e];
-        store8<SPLIT>(ws + M.x + chunk_at<SPLIT>(M.row_n, i0 + a, j0 + c), v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = tile[c + e][a];
-        store8<SPLIT>(ws + M.xt[0] + chunk_at<SPLIT>(M.row_m, j0 + a, i0 + c), v);
+        store8<SPLIT>(ws + M.x[0] + chunk_at<SPLIT>(M.row_n, i0 + a, j0 + c), v);
     }
 }
 
@@ -179,7 +197,7 @@ enum Stage { kGram, kPoly, kApply, kLast };    // G = X X' ; B = b G + c G G ; X
 
 struct Step {
     float a, b, c;
-    int from;                  // which of the two transposed copies holds X'
+    int from;                  // which of the two X the step starts from
 };
 
 // Where the last product goes.
@@ -189,117 +207,196 @@ struct Out {
     float keep, gamma;
 };
 
-template <int T, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
-__global__ __launch_bounds__(kThreads) void k_ortho_product(const Mat *__restrict__ mats, const Tile *__restrict__ tiles, char *ws,
-                                                            Step step, Out out)
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// Direct copy of 16 bytes per lane into LDS, lane l to `lds` + 16 l; `lds` is the same for the wavefront.  It has no output
+// register.  Written as an instruction because the compiler waits for every outstanding copy of its own builtin before
+// the next read of LDS, also of the other stage; the wait that is needed stands in front of the barrier of that stage.
+__device__ __forceinline__ void copy_to_lds(const char *from, uint32_t lds)
 {
-    constexpr int W = T / 2, F = W / 32;            // a wavefront's part of the tile, in 32 x 32 products
-    constexpr int STRIDE = kRowBlock + 16;
-    __shared__ __attribute__((aligned(16))) char lds[2 * T * STRIDE > T * (T + 1) * 4 ? 2 * T * STRIDE : T * (T + 1) * 4];
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds) : "memory", "m0");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p)
+{
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)p));
+}
+
+__device__ __forceinline__ f32x16 mfma(half8 a, half8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// One tile of TM x TN of C = P Q, by wavefronts of WM x WN.  P is read by rows of k (blocks of 128 bytes).  Q = X' or G
+// (symmetric) is read by rows of k as well; Q = X, in the last product, lies as rows of j under each other, k = row: its tile
+// is transposed on the way from LDS to the registers.
+//
+// LDS: two stages; while one is multiplied, the next is copied in without passing the registers.  LDS has 64 banks, 256
+// bytes; a copy fills it linearly, so what a lane copies is chosen such that the 16-byte chunk c of row r lies at c ^ f(r),
+// and 16 lanes that read 16 rows of one chunk (or, transposing, 32 lanes 4 rows of 4 chunks) meet different banks: 267 and 228
+// bytes a clock measured, 43 and 80 without.
+//
+// The wavefront multiplies Q' P': a lane then holds a row i of C and four consecutive j at a time.
+template <int TM, int TN, int WM, int WN, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
+__global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Mat *__restrict__ mats, const Tile *__restrict__ tiles,
+                                                                             char *ws, Step step, Out out)
+{
+    constexpr int WAVES_N = TN / WN, WAVES = (TM / WM) * WAVES_N, FM = WM / 32, FN = WN / 32;
+    constexpr bool ROWS = STAGE >= kApply;                     // Q is X
+    constexpr int KROWS = SPLIT ? 32 : 64;                     // values of k in a stage
+    constexpr int QROW = SPLIT ? TN * 4 : TN * 2;              // bytes of one of its rows in LDS
+    constexpr int PBYTES = TM * kRowBlock, QBYTES = TN * kRowBlock, STAGE_BYTES = PBYTES + QBYTES;
+    constexpr int PCOPIES = PBYTES / (WAVES * 1024), QCOPIES = QBYTES / (WAVES * 1024);
+    static_assert(PCOPIES * WAVES * 1024 == PBYTES && QCOPIES * WAVES * 1024 == QBYTES && QROW * KROWS == QBYTES, "tile");
+    __shared__ __attribute__((aligned(256))) char lds[2 * STAGE_BYTES];
     const Tile tl = tiles[blockIdx.x];
     const Mat &M = mats[tl.mat];
-    const int i0 = tl.i * T, j0 = tl.j * T;
+    const int i0 = tl.i * TM, j0 = tl.j * TN;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int wi = (wave / WAVES_N) * WM, wj = (wave % WAVES_N) * WN;
     const int64_t row_k = STAGE == kGram ? M.row_n : M.row_m;
-    const char *P = ws + (STAGE == kGram ? M.x : STAGE == kPoly ? M.g : M.b) + i0 * row_k;
-    const char *Q = ws + (STAGE == kGram ? M.x : STAGE == kPoly ? M.g : M.xt[step.from]) + j0 * row_k;
-    const int lane = lane_id(), wave = wave_id();
-    const int wi = (wave >> 1) * W, wj = (wave & 1) * W;
-    f32x16 acc[F][F];
+    const int steps_k = static_cast<int>(row_k / kRowBlock);
+    const char *X = ws + M.x[step.from];
+    const char *P = STAGE == kGram ? X : ws + (STAGE == kPoly ? M.g : M.b);
+    const char *Q = ROWS ? X : P;
+    // what this lane copies; a tile may reach past the rounded matrix, whose last rows then stand in for what is not there
+    const char *pa[PCOPIES], *qa[QCOPIES];
 #pragma unroll
-    for (int a = 0; a < F; ++a)
+    for (int t = 0; t < PCOPIES; ++t) {
+        const int at = (t * WAVES + wave) * 1024 + lane * 16, r = at / kRowBlock, c = ((at % kRowBlock) / 16) ^ ((r >> 1) & 7);
+        const int row = i0 + r < M.mp ? i0 + r : M.mp - 1;
+        pa[t] = P + row * row_k + c * 16;
+    }
 #pragma unroll
-        for (int b = 0; b < F; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
-    char *lp = lds, *lq = lds + T * STRIDE;
-    for (int64_t k = 0; k < row_k; k += kRowBlock) {
-        for (int t = threadIdx.x; t < T * 8; t += kThreads) {
-            const int r = t >> 3, c = (t & 7) * 16;
-            *reinterpret_cast<u32x4 *>(lp + r * STRIDE + c) = *reinterpret_cast<const u32x4 *>(P + r * row_k + k + c);
-            *reinterpret_cast<u32x4 *>(lq + r * STRIDE + c) = *reinterpret_cast<const u32x4 *>(Q + r * row_k + k + c);
+    for (int t = 0; t < QCOPIES; ++t) {
+        const int at = (t * WAVES + wave) * 1024 + lane * 16;
+        if (ROWS) {
+            const int r = at / QROW, f = QROW == 128 ? 4 * ((r >> 1) & 1) : 4 * (r & 3);
+            const int byte = static_cast<int>(j0 * (SPLIT ? 4 : 2)) + ((((at % QROW) / 16) ^ f) * 16);
+            qa[t] = Q + r * static_cast<int64_t>(M.row_n) + (byte < M.row_n ? byte : M.row_n - 16);
+        } else {
+            const int r = at / kRowBlock, c = ((at % kRowBlock) / 16) ^ ((r >> 1) & 7);
+            const int row = j0 + r < M.mp ? j0 + r : M.mp - 1;
+            qa[t] = Q + row * row_k + c * 16;
         }
-        __syncthreads();
-        // lane l holds row l % 32, values 8 (l / 32) .. + 7 of the 16 that one instruction takes
+    }
+    const int64_t q_step = ROWS ? static_cast<int64_t>(M.row_n) * KROWS : kRowBlock;
+    const uint32_t lds_at = __builtin_amdgcn_readfirstlane(lds_address(lds));
+    auto copy = [&](int stage) {
+        const uint32_t to = lds_at + stage * STAGE_BYTES + wave * 1024;
 #pragma unroll
-        for (int s = 0; s < (SPLIT ? 2 : 4); ++s) {
-            half8 ph[F], pl[F], qh[F], ql[F];
+        for (int t = 0; t < PCOPIES; ++t) {
+            copy_to_lds(pa[t], to + t * WAVES * 1024);
+            pa[t] += kRowBlock;
+        }
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                const char *pr = lp + (wi + f * 32 + (lane & 31)) * STRIDE + s * 32 + (lane >> 5) * 16;
-                const char *qr = lq + (wj + f * 32 + (lane & 31)) * STRIDE + s * 32 + (lane >> 5) * 16;
-                ph[f] = *reinterpret_cast<const half8 *>(pr);
-                qh[f] = *reinterpret_cast<const half8 *>(qr);
-                if (SPLIT) {
-                    pl[f] = *reinterpret_cast<const half8 *>(pr + kRowBlock / 2);
-                    ql[f] = *reinterpret_cast<const half8 *>(qr + kRowBlock / 2);
-                }
+        for (int t = 0; t < QCOPIES; ++t) {
+            copy_to_lds(qa[t], to + PBYTES + t * WAVES * 1024);
+            qa[t] += q_step;
+        }
+    };
+    // fragments: row r of 32, values 8 h .. 8 h + 7 of the 16 of step s, plane lo or hi
+    const int r = lane & 31, h = lane >> 5;
+    auto by_rows = [&](const char *tile, int row, int s, int plane) {
+        const int c = SPLIT ? plane * 4 + s * 2 + h : s * 2 + h;
+        return *reinterpret_cast<const half8 *>(tile + (row + r) * kRowBlock + ((c ^ (((row + r) >> 1) & 7)) * 16));
+    };
+    auto by_columns = [&](const char *tile, int col0, int s, int plane) {
+        union { half8 v; s16x4 part[2]; } u;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int k = s * 16 + h * 8 + q * 4 + ((lane & 15) >> 2), col = col0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+            const int c = SPLIT ? (col >> 5) * 8 + plane * 4 + ((col & 31) >> 3) : col >> 3;
+            const int f = QROW == 128 ? 4 * ((k >> 1) & 1) : 4 * (k & 3);
+            u.part[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + k * QROW + ((c ^ f) * 16) + (col & 7) * 2));
+        }
+        return u.v;
+    };
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int a = 0; a < FM; ++a)
+#pragma unroll
+        for (int b = 0; b < FN; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.f;
+    copy(0);
+    for (int k = 0; k < steps_k; ++k) {
+        const int stage = k & 1;
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");     // this wavefront's copies into `stage` are there
+        __syncthreads();                                       // everybody's, and nobody reads the other stage any more
+        if (k + 1 < steps_k) copy(1 - stage);
+        const char *lp = lds + stage * STAGE_BYTES, *lq = lp + PBYTES;
+#pragma unroll
+        for (int s = 0; s < KROWS / 16; ++s) {
+            half8 ph[FM], pl[FM], qh[FN], ql[FN];
+#pragma unroll
+            for (int a = 0; a < FM; ++a) {
+                ph[a] = by_rows(lp, wi + a * 32, s, 0);
+                if (SPLIT) pl[a] = by_rows(lp, wi + a * 32, s, 1);
             }
 #pragma unroll
-            for (int a = 0; a < F; ++a)
+            for (int b = 0; b < FN; ++b) {
+                qh[b] = ROWS ? by_columns(lq, wj + b * 32, s, 0) : by_rows(lq, wj + b * 32, s, 0);
+                if (SPLIT) ql[b] = ROWS ? by_columns(lq, wj + b * 32, s, 1) : by_rows(lq, wj + b * 32, s, 1);
+            }
 #pragma unroll
-                for (int b = 0; b < F; ++b) {
+            for (int a = 0; a < FM; ++a)
+#pragma unroll
+                for (int b = 0; b < FN; ++b) {
                     if (SPLIT) {
-                        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[a], qh[b], acc[a][b], 0, 0, 0);
-                        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], ql[b], acc[a][b], 0, 0, 0);
+                        acc[a][b] = mfma(qh[b], pl[a], acc[a][b]);
+                        acc[a][b] = mfma(ql[b], ph[a], acc[a][b]);
                     }
-                    acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], qh[b], acc[a][b], 0, 0, 0);
+                    acc[a][b] = mfma(qh[b], ph[a], acc[a][b]);
                 }
         }
-        __syncthreads();
     }
-    // lane l holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4
-    float (*ct)[T + 1] = reinterpret_cast<float (*)[T + 1]>(lds);
-#pragma unroll
-    for (int a = 0; a < F; ++a)
-#pragma unroll
-        for (int b = 0; b < F; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                ct[wi + a * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)][wj + b * 32 + (lane & 31)] = acc[a][b][r];
-    __syncthreads();
     // the product's scale away, the stage's scale on
     const float alpha = STAGE == kGram ? kGramScale / (M.scale * M.scale)
                         : STAGE == kPoly ? step.c * (kPolyScale / (kGramScale * kGramScale)) : 1.0f / kPolyScale;
     const float beta = STAGE == kGram ? 0.f : STAGE == kPoly ? step.b * (kPolyScale / kGramScale) : step.a;
-    const int64_t row_c = STAGE >= kApply ? M.row_n : M.row_m;
-    const char *old = ws + (STAGE == kPoly ? M.g : M.x);
-    char *to = ws + (STAGE == kGram ? M.g : STAGE == kPoly ? M.b : M.x);
-    for (int t = threadIdx.x; t < T * T / 8; t += kThreads) {
-        const int r = t / (T / 8), c = (t % (T / 8)) * 8;
-        float v[8];
-        const int64_t at = chunk_at<SPLIT>(row_c, i0 + r, j0 + c);
-        if (STAGE != kGram) load8<SPLIT>(old + at, v);
+    const int64_t row_c = ROWS ? M.row_n : M.row_m;
+    const int j_end = ROWS ? M.np : M.mp;
+    const char *old = STAGE == kPoly ? P : X;
+    char *to = ws + (STAGE == kGram ? M.g : STAGE == kPoly ? M.b : M.x[1 - step.from]);
+    const float f = M.factor / M.scale;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float p = ct[r][c + e] * alpha;
-            v[e] = STAGE == kGram ? p : __fmaf_rn(beta, v[e], p);
-            ct[r][c + e] = v[e];
-        }
-        if (STAGE != kLast) store8<SPLIT>(to + at, v);
-    }
-    if (STAGE < kApply && tl.i == tl.j) return;
-    __syncthreads();
-    if constexpr (STAGE != kLast) {
-        char *tt = ws + (STAGE == kGram ? M.g : STAGE == kPoly ? M.b : M.xt[1 - step.from]);
-        for (int t = threadIdx.x; t < T * T / 8; t += kThreads) {
-            const int r = t / (T / 8), c = (t % (T / 8)) * 8;
-            float v[8];
+    for (int a = 0; a < FM; ++a) {
+        const int i = i0 + wi + a * 32 + r;
+        if (i0 + wi + a * 32 >= M.mp) break;                   // rounded sizes are multiples of 64: whole 32 x 32 parts
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = ct[c + e][r];
-            store8<SPLIT>(tt + chunk_at<SPLIT>(M.row_m, j0 + r, i0 + c), v);
-        }
-    } else {
-        const float f = M.factor / M.scale;
-        for (int t = threadIdx.x; t < T * T; t += kThreads) {
-            const int fast = t & (T - 1), slow = t / T;
-            const int i = M.flip ? fast : slow, j = M.flip ? slow : fast;
-            if (i0 + i >= M.m || j0 + j >= M.n) continue;
-            const int64_t r = M.flip ? j0 + j : i0 + i, c = M.flip ? i0 + i : j0 + j;
-            const int64_t at = M.offset + r * M.ld + c;
-            const float o = ct[i][j] * f;
-            if (OUT == 0) static_cast<float *>(out.dst)[at] = o;
-            else if (OUT == 1) static_cast<uint16_t *>(out.dst)[at] = bf16_round(o);
-            else out.x[at] = __fmaf_rn(-out.gamma, o, out.keep * out.x[at]);
+        for (int b = 0; b < FN; ++b) {
+            const int jb = j0 + wj + b * 32;
+            if (jb >= j_end) break;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int j = jb + 8 * g + 4 * h;
+                const int64_t at = chunk_at<SPLIT>(row_c, i, j);
+                float v[4];
+                if (STAGE != kGram) load4<SPLIT>(old + at, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = acc[a][b][4 * g + e] * alpha;
+                    v[e] = STAGE == kGram ? p : __fmaf_rn(beta, v[e], p);
+                }
+                if constexpr (STAGE != kLast) {
+                    store4<SPLIT>(to + at, v);
+                    if (STAGE < kApply && tl.i != tl.j) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) store1<SPLIT>(to + chunk_at<SPLIT>(row_c, j + e, i & ~7) + (i & 7) * 2, v[e]);
+                    }
+                } else if (i < M.m) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (j + e >= M.n) break;
+                        const int64_t o_at = M.offset + (M.flip ? (j + e) * M.ld + i : i * M.ld + j + e);
+                        const float o = v[e] * f;
+                        if (OUT == 0) static_cast<float *>(out.dst)[o_at] = o;
+                        else if (OUT == 1) static_cast<uint16_t *>(out.dst)[o_at] = bf16_round(o);
+                        else out.x[o_at] = __fmaf_rn(-out.gamma, o, out.keep * out.x[o_at]);
+                    }
+                }
+            }
         }
     }
 }
@@ -318,6 +415,7 @@ struct ds_ortho {
     const Tile *square, *wide, *operands;  // tiles of G and B, of X, and of the operands' pass
     const int2 *parts;
     int64_t n_square, n_wide, n_operands, n_parts;
+    int square_side, wide_side;
     double *partial;
     uint64_t *inside;                      // plane of bits: the elements of the matrices
     float *u;                              // [d] what is orthogonalised, where it is not m
@@ -348,7 +446,66 @@ struct Tables {
     std::vector<Tile> square, wide, operands;
     std::vector<int2> parts;
     int64_t n_partial = 0, ws_bytes = 0;
+    int square_side = 64, wide_side = 64;
 };
+
+// Tiles of `side` in the order in which they are given out: long sums first, so that the launch ends with short ones; within a
+// matrix strips of rows, so that tiles near each other in time share rows and columns; runs of kRun tiles to one XCD
+// (workgroup p runs on XCD p % 8, each with an L2 of its own).
+std::vector<Tile> make_tiles(const std::vector<Mat> &mats, int side, bool square)
+{
+    constexpr size_t kRun = 32;
+    std::vector<int32_t> order(mats.size());
+    for (size_t k = 0; k < mats.size(); ++k) order[k] = static_cast<int32_t>(k);
+    auto length = [&](int32_t k) { return square ? mats[k].np : mats[k].mp; };
+    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return length(a) > length(b); });
+    std::vector<Tile> list;
+    const int32_t strip = 1024 / side;
+    for (int32_t k : order) {
+        const int32_t ti = (mats[k].mp + side - 1) / side, tj = square ? ti : (mats[k].np + side - 1) / side;
+        for (int32_t i0 = 0; i0 < ti; i0 += strip)
+            for (int32_t j = 0; j < tj; ++j)
+                for (int32_t i = i0; i < std::min(i0 + strip, ti); ++i)
+                    if (!square || j <= i) list.push_back(Tile{k, i, j, 0});
+    }
+    std::vector<Tile> out;
+    out.reserve(list.size());
+    size_t next[8], xcd = 0;
+    for (size_t q = 0; q < 8; ++q) next[q] = q * kRun;
+    while (out.size() < list.size()) {
+        if (next[xcd] < list.size()) {
+            out.push_back(list[next[xcd]]);
+            if (++next[xcd] % kRun == 0) next[xcd] += 7 * kRun;
+        } else {
+            // nothing is left for this XCD: its turn goes to the one that has most left
+            size_t far = 8;
+            for (size_t q = 0; q < 8; ++q)
+                if (next[q] < list.size() && (far == 8 || next[q] < next[far])) far = q;
+            out.push_back(list[next[far]]);
+            if (++next[far] % kRun == 0) next[far] += 7 * kRun;
+        }
+        xcd = (xcd + 1) % 8;
+    }
+    return out;
+}
+
+int64_t count_tiles(const std::vector<Mat> &mats, int side, bool square)
+{
+    int64_t n = 0;
+    for (const Mat &M : mats) {
+        const int64_t ti = (M.mp + side - 1) / side, tj = (M.np + side - 1) / side;
+        n += square ? ti * (ti + 1) / 2 : ti * tj;
+    }
+    return n;
+}
+
+// Side of the tiles: rounds of the device's 256 compute units times the time of a tile.
+int tile_side(const std::vector<Mat> &mats, bool square)
+{
+    auto rounds = [&](int side, int64_t at_once) { return static_cast<double>((count_tiles(mats, side, square) + at_once - 1) / at_once); };
+    const double t256 = rounds(256, 256) * 1.0, t128 = rounds(128, 512) * 0.55, t64 = rounds(64, 1024) * 0.35;
+    return t64 < t128 && t64 < t256 ? 64 : t128 < t256 ? 128 : 256;
+}
 
 void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
 {
@@ -379,9 +536,8 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
             t.ws_bytes += round_up(bytes, 256);
             return at;
         };
-        M.x = take(static_cast<int64_t>(M.mp) * M.row_n);
-        M.xt[0] = take(static_cast<int64_t>(M.np) * M.row_m);
-        M.xt[1] = take(static_cast<int64_t>(M.np) * M.row_m);
+        M.x[0] = take(static_cast<int64_t>(M.mp) * M.row_n);
+        M.x[1] = take(static_cast<int64_t>(M.mp) * M.row_n);
         M.g = take(static_cast<int64_t>(M.mp) * M.row_m);
         M.b = take(static_cast<int64_t>(M.mp) * M.row_m);
         const int64_t elements = static_cast<int64_t>(M.m) * M.n;
@@ -389,14 +545,26 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
         M.part0 = static_cast<int32_t>(t.n_partial);
         t.n_partial += M.parts;
         for (int32_t p = 0; p < M.parts; ++p) t.parts.push_back(int2{k, p});
-        const int32_t ti = M.mp / kTileSide, tj = M.np / kTileSide;
-        for (int32_t i = 0; i < ti; ++i)
-            for (int32_t j = 0; j <= i; ++j) t.square.push_back(Tile{k, i, j, 0});
-        for (int32_t j = 0; j < tj; ++j)
-            for (int32_t i = 0; i < ti; ++i) t.wide.push_back(Tile{k, i, j, 0});
         t.mats.push_back(M);
     }
-    t.operands = t.wide;
+    t.square_side = tile_side(t.mats, true);
+    t.wide_side = tile_side(t.mats, false);
+    t.square = make_tiles(t.mats, t.square_side, true);
+    t.wide = make_tiles(t.mats, t.wide_side, false);
+    t.operands = make_tiles(t.mats, 64, false);
+}
+
+template <bool SPLIT, int STAGE, int OUT>
+void product(const ds_ortho *o, const Step &s, const Out &out, hipStream_t st)
+{
+    constexpr bool WIDE = STAGE >= kApply;
+    const Tile *tiles = WIDE ? o->wide : o->square;
+    const unsigned n = static_cast<unsigned>(WIDE ? o->n_wide : o->n_square);
+    switch (WIDE ? o->wide_side : o->square_side) {
+    case 256: k_ortho_product<256, 256, 128, 64, SPLIT, STAGE, OUT><<<n, 512, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
+    case 128: k_ortho_product<128, 128, 64, 64, SPLIT, STAGE, OUT><<<n, 256, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
+    default: k_ortho_product<64, 64, 32, 32, SPLIT, STAGE, OUT><<<n, 256, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
+    }
 }
 
 // The matrices through the plan's steps; `src` holds U, where the last product goes is `out`.
@@ -408,12 +576,10 @@ ds_status_t run(const ds_ortho *o, const void *src, const Out &out, hipStream_t 
     k_ortho_operands<SPLIT, SRC_BF16><<<grid(o->n_operands), kThreads, 0, st>>>(o->mats, o->operands, src, o->partial, o->cfg.eps, o->ws);
     for (int32_t k = 0; k < o->cfg.steps; ++k) {
         const Step s{o->coef[3 * k], o->coef[3 * k + 1], o->coef[3 * k + 2], k & 1};
-        k_ortho_product<kTileSide, SPLIT, kGram, 0><<<grid(o->n_square), kThreads, 0, st>>>(o->mats, o->square, o->ws, s, out);
-        k_ortho_product<kTileSide, SPLIT, kPoly, 0><<<grid(o->n_square), kThreads, 0, st>>>(o->mats, o->square, o->ws, s, out);
-        if (k + 1 < o->cfg.steps)
-            k_ortho_product<kTileSide, SPLIT, kApply, 0><<<grid(o->n_wide), kThreads, 0, st>>>(o->mats, o->wide, o->ws, s, out);
-        else
-            k_ortho_product<kTileSide, SPLIT, kLast, OUT><<<grid(o->n_wide), kThreads, 0, st>>>(o->mats, o->wide, o->ws, s, out);
+        product<SPLIT, kGram, 0>(o, s, out, st);
+        product<SPLIT, kPoly, 0>(o, s, out, st);
+        if (k + 1 < o->cfg.steps) product<SPLIT, kApply, 0>(o, s, out, st);
+        else product<SPLIT, kLast, OUT>(o, s, out, st);
     }
     return ds_launch_status();
 }
@@ -484,6 +650,8 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
         o->n_wide = static_cast<int64_t>(t.wide.size());
         o->n_operands = static_cast<int64_t>(t.operands.size());
         o->n_parts = static_cast<int64_t>(t.parts.size());
+        o->square_side = t.square_side;
+        o->wide_side = t.wide_side;
         int64_t bytes = 0;
         auto take = [&](int64_t b) {
             const int64_t at = bytes;
