@@ -14,7 +14,9 @@
 // With one half (DS_ORTHO_HALF) a rounding is 2^-11 at most; it grows with the smallest singular values at most, 3.44^5 = 485 times
 // while an entry of X grows as much or reaches 1 / sqrt(n), so it ends below a rounding to bf16.
 //
-// Layout.  A row of an operand is a sequence of 128-byte blocks: 32 values as 32 hi and 32 lo, or 64 values with one half.
+// Layout.  An operand lies in panels of 16 columns (32 with one half): row after row 64 bytes, 16 hi and 16 lo (32 halves).  A
+// stage of a product, 16 (32) values of k, is then one contiguous piece of a tile's rows when k runs along the rows, and
+// pieces of 1 KB (2 KB) when k runs across them.
 #include "ds_device.h"
 #include "ds_internal.h"
 #include "tails.h"
@@ -23,6 +25,7 @@
 
 #include <algorithm>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 using namespace ds;
@@ -35,7 +38,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
-constexpr int kRowBlock = 128;                 // bytes of one block of a row
+constexpr int kRow = 64;                       // bytes of a row in a panel
 constexpr float kGramScale = 8192.0f;          // G is held times 2^13 (entries up to 8)
 constexpr float kPolyScale = 4096.0f;          // B is held times 2^12 (entries up to 16)
 constexpr int kTileSide = 64;
@@ -47,12 +50,11 @@ struct Mat {
     int64_t x[2], g, b;          // byte offsets in the workspace
     int32_t rows, cols;          // as stored
     int32_t m, n, mp, np;        // as worked on: m <= n, and rounded up to tiles
-    int32_t row_n, row_m;        // bytes of a row of np and of mp values
+    int32_t panel;               // bytes of a panel: mp rows
     int32_t flip;                // stored transposed
     int32_t part0, parts;        // partial sums of the norm
     float scale;                 // X is held times this
     float factor;
-    int32_t pad_;
 };
 
 struct Tile {
@@ -60,10 +62,17 @@ struct Tile {
 };
 
 template <bool SPLIT>
-__device__ __forceinline__ int64_t chunk_at(int64_t row_bytes, int row, int k)     // k a multiple of 4
+constexpr int kPanel = SPLIT ? 16 : 32;        // columns of a panel
+
+// Byte of element (row, col) of an operand, of its hi where there are two.
+template <bool SPLIT>
+__device__ __forceinline__ int64_t element_at(int64_t panel, int row, int col)
 {
-    return row * row_bytes + (SPLIT ? (k >> 5) * kRowBlock + (k & 31) * 2 : k * 2);
+    constexpr int W = kPanel<SPLIT>;
+    return (col / W) * panel + row * kRow + (col % W) * 2;
 }
+
+constexpr int kToLo = kRow / 2;                // from hi to lo
 
 template <bool SPLIT>
 __device__ __forceinline__ void store8(char *p, const float *v)
@@ -75,20 +84,7 @@ __device__ __forceinline__ void store8(char *p, const float *v)
         lo[t] = static_cast<_Float16>(v[t] - static_cast<float>(hi[t]));
     }
     *reinterpret_cast<half8 *>(p) = hi;
-    if (SPLIT) *reinterpret_cast<half8 *>(p + kRowBlock / 2) = lo;
-}
-
-template <bool SPLIT>
-__device__ __forceinline__ void store4(char *p, const float *v)
-{
-    half4 hi, lo;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        hi[t] = static_cast<_Float16>(v[t]);
-        lo[t] = static_cast<_Float16>(v[t] - static_cast<float>(hi[t]));
-    }
-    *reinterpret_cast<half4 *>(p) = hi;
-    if (SPLIT) *reinterpret_cast<half4 *>(p + kRowBlock / 2) = lo;
+    if (SPLIT) *reinterpret_cast<half8 *>(p + kToLo) = lo;
 }
 
 template <bool SPLIT>
@@ -96,19 +92,19 @@ __device__ __forceinline__ void store1(char *p, float v)
 {
     const _Float16 hi = static_cast<_Float16>(v);
     *reinterpret_cast<_Float16 *>(p) = hi;
-    if (SPLIT) *reinterpret_cast<_Float16 *>(p + kRowBlock / 2) = static_cast<_Float16>(v - static_cast<float>(hi));
+    if (SPLIT) *reinterpret_cast<_Float16 *>(p + kToLo) = static_cast<_Float16>(v - static_cast<float>(hi));
 }
 
 template <bool SPLIT>
-__device__ __forceinline__ void load4(const char *p, float *v)
+__device__ __forceinline__ void load8(const char *p, float *v)
 {
-    const half4 hi = *reinterpret_cast<const half4 *>(p);
+    const half8 hi = *reinterpret_cast<const half8 *>(p);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = static_cast<float>(hi[t]);
+    for (int t = 0; t < 8; ++t) v[t] = static_cast<float>(hi[t]);
     if (SPLIT) {
-        const half4 lo = *reinterpret_cast<const half4 *>(p + kRowBlock / 2);
+        const half8 lo = *reinterpret_cast<const half8 *>(p + kToLo);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) v[t] += static_cast<float>(lo[t]);
+        for (int t = 0; t < 8; ++t) v[t] += static_cast<float>(lo[t]);
     }
 }
 
@@ -186,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_operands(const Mat *__restri
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = tile[a][c + e];
-        store8<SPLIT>(ws + M.x[0] + chunk_at<SPLIT>(M.row_n, i0 + a, j0 + c), v);
+        store8<SPLIT>(ws + M.x[0] + element_at<SPLIT>(M.panel, i0 + a, j0 + c), v);
     }
 }
 
@@ -209,12 +205,13 @@ struct Out {
 
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// Direct copy of 16 bytes per lane into LDS, lane l to `lds` + 16 l; `lds` is the same for the wavefront.  It has no output
-// register.  Written as an instruction because the compiler waits for every outstanding copy of its own builtin before
-// the next read of LDS, also of the other stage; the wait that is needed stands in front of the barrier of that stage.
-__device__ __forceinline__ void copy_to_lds(const char *from, uint32_t lds)
+// Direct copy of 16 bytes per lane, from `base` + `offset` into LDS at `lds` + 16 l for lane l; `base` and `lds` are the same for
+// the wavefront.  It has no output register.  Written as an instruction because the compiler waits for every
+// outstanding copy of its own builtin before the next read of LDS, also of another stage; the wait that is needed
+// stands in front of the barrier of that stage.
+__device__ __forceinline__ void copy_to_lds(const char *base, uint32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory", "m0");
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void *p)
@@ -227,90 +224,109 @@ __device__ __forceinline__ f32x16 mfma(half8 a, half8 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// One tile of TM x TN of C = P Q, by wavefronts of WM x WN.  P is read by rows of k (blocks of 128 bytes).  Q = X' or G
-// (symmetric) is read by rows of k as well; Q = X, in the last product, lies as rows of j under each other, k = row: its tile
-// is transposed on the way from LDS to the registers.
+template <int N>
+__device__ __forceinline__ void wait_copies()       // at most N copies of this wavefront under way, and its reads of LDS are done
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
+}
+
+// One tile of TM x TN of C = P Q, by wavefronts of WM x WN.  P is read by rows of k.  Q = X' or G (symmetric) is read by rows
+// of k as well; Q = X, in the last product, lies with k across the rows: its tile is transposed on the way from LDS to the
+// registers.
 //
-// LDS: two stages; while one is multiplied, the next is copied in without passing the registers.  LDS has 64 banks, 256
-// bytes; a copy fills it linearly, so what a lane copies is chosen such that the 16-byte chunk c of row r lies at c ^ f(r),
-// and 16 lanes that read 16 rows of one chunk (or, transposing, 32 lanes 4 rows of 4 chunks) meet different banks: 267 and 228
-// bytes a clock measured, 43 and 80 without.
+// Pipeline.  LDS holds S stages of 16 (32) values of k.  While stage k is multiplied from registers, the fragments of stage k
+// + 1 are read from LDS and the copies of stages k + 2 .. k + S, which pass no registers, are under way; one barrier a stage.
+//
+// LDS has 64 banks, 256 bytes.  A copy fills it linearly, so what a lane copies is chosen such that the 16-byte chunk c of
+// row r lies at c ^ f(r), and 16 lanes that read 16 rows of one chunk (or, transposing, 32 lanes 4 rows of 4 chunks) meet
+// different banks: 267 and 228 bytes a clock measured, 43 and 80 without.
 //
 // The wavefront multiplies Q' P': a lane then holds a row i of C and four consecutive j at a time.
-template <int TM, int TN, int WM, int WN, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
+template <int TM, int TN, int WM, int WN, int S, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
 __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Mat *__restrict__ mats, const Tile *__restrict__ tiles,
                                                                              char *ws, Step step, Out out)
 {
     constexpr int WAVES_N = TN / WN, WAVES = (TM / WM) * WAVES_N, FM = WM / 32, FN = WN / 32;
-    constexpr bool ROWS = STAGE >= kApply;                     // Q is X
-    constexpr int KROWS = SPLIT ? 32 : 64;                     // values of k in a stage
-    constexpr int QROW = SPLIT ? TN * 4 : TN * 2;              // bytes of one of its rows in LDS
-    constexpr int PBYTES = TM * kRowBlock, QBYTES = TN * kRowBlock, STAGE_BYTES = PBYTES + QBYTES;
-    constexpr int PCOPIES = PBYTES / (WAVES * 1024), QCOPIES = QBYTES / (WAVES * 1024);
-    static_assert(PCOPIES * WAVES * 1024 == PBYTES && QCOPIES * WAVES * 1024 == QBYTES && QROW * KROWS == QBYTES, "tile");
-    __shared__ __attribute__((aligned(256))) char lds[2 * STAGE_BYTES];
+    constexpr bool ACROSS = STAGE >= kApply;                   // Q is X
+    constexpr int K = kPanel<SPLIT>, PIECE = K * kRow;         // values of k in a stage; a panel's part of a stage of X
+    constexpr int PBYTES = TM * kRow, QBYTES = TN * kRow, STAGE_BYTES = PBYTES + QBYTES;
+    constexpr int PCOPIES = PBYTES / (WAVES * 1024), QCOPIES = QBYTES / (WAVES * 1024), COPIES = PCOPIES + QCOPIES;
+    static_assert(PCOPIES * WAVES * 1024 == PBYTES && QCOPIES * WAVES * 1024 == QBYTES && S >= 3, "tile");
+    __shared__ __attribute__((aligned(256))) char lds[S * STAGE_BYTES];
     const Tile tl = tiles[blockIdx.x];
     const Mat &M = mats[tl.mat];
-    const int i0 = tl.i * TM, j0 = tl.j * TN;
+    const int i0 = tl.i * TM, j0 = tl.j * TN, mp = M.mp, np = M.np;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int wi = (wave / WAVES_N) * WM, wj = (wave % WAVES_N) * WN;
-    const int64_t row_k = STAGE == kGram ? M.row_n : M.row_m;
-    const int steps_k = static_cast<int>(row_k / kRowBlock);
+    const int64_t panel = M.panel;
+    const int stages = (STAGE == kGram ? np : mp) / K;         // even: rounded sizes are multiples of 64
     const char *X = ws + M.x[step.from];
     const char *P = STAGE == kGram ? X : ws + (STAGE == kPoly ? M.g : M.b);
-    const char *Q = ROWS ? X : P;
+    const char *Q = ACROSS ? X : P;
     // what this lane copies; a tile may reach past the rounded matrix, whose last rows then stand in for what is not there
-    const char *pa[PCOPIES], *qa[QCOPIES];
+    uint32_t pa[PCOPIES], qa[QCOPIES];
+    const char *p_base = P, *q_base = ACROSS ? Q + (j0 / K) * panel : Q;
 #pragma unroll
     for (int t = 0; t < PCOPIES; ++t) {
-        const int at = (t * WAVES + wave) * 1024 + lane * 16, r = at / kRowBlock, c = ((at % kRowBlock) / 16) ^ ((r >> 1) & 7);
-        const int row = i0 + r < M.mp ? i0 + r : M.mp - 1;
-        pa[t] = P + row * row_k + c * 16;
+        const int at = (t * WAVES + wave) * 1024 + lane * 16, r = at / kRow, c = ((at % kRow) / 16) ^ ((r >> 2) & 3);
+        pa[t] = (i0 + r < mp ? i0 + r : mp - 1) * kRow + c * 16;
     }
 #pragma unroll
     for (int t = 0; t < QCOPIES; ++t) {
         const int at = (t * WAVES + wave) * 1024 + lane * 16;
-        if (ROWS) {
-            const int r = at / QROW, f = QROW == 128 ? 4 * ((r >> 1) & 1) : 4 * (r & 3);
-            const int byte = static_cast<int>(j0 * (SPLIT ? 4 : 2)) + ((((at % QROW) / 16) ^ f) * 16);
-            qa[t] = Q + r * static_cast<int64_t>(M.row_n) + (byte < M.row_n ? byte : M.row_n - 16);
+        if (ACROSS) {
+            const int b = at / PIECE, r = (at % PIECE) / kRow, c = ((at % kRow) / 16) ^ (SPLIT ? 2 * (b & 1) : 0);
+            const int last = (np - j0) / K - 1;
+            qa[t] = static_cast<uint32_t>(b < last ? b : last) * M.panel + r * kRow + c * 16;
         } else {
-            const int r = at / kRowBlock, c = ((at % kRowBlock) / 16) ^ ((r >> 1) & 7);
-            const int row = j0 + r < M.mp ? j0 + r : M.mp - 1;
-            qa[t] = Q + row * row_k + c * 16;
+            const int r = at / kRow, c = ((at % kRow) / 16) ^ ((r >> 2) & 3);
+            qa[t] = (j0 + r < mp ? j0 + r : mp - 1) * kRow + c * 16;
         }
     }
-    const int64_t q_step = ROWS ? static_cast<int64_t>(M.row_n) * KROWS : kRowBlock;
-    const uint32_t lds_at = __builtin_amdgcn_readfirstlane(lds_address(lds));
-    auto copy = [&](int stage) {
-        const uint32_t to = lds_at + stage * STAGE_BYTES + wave * 1024;
+    const int64_t q_step = ACROSS ? PIECE : panel;
+    const uint32_t lds_at = __builtin_amdgcn_readfirstlane(lds_address(lds)) + wave * 1024;
+    auto copy = [&](int buffer) {
+        const uint32_t to = lds_at + buffer * STAGE_BYTES;
 #pragma unroll
-        for (int t = 0; t < PCOPIES; ++t) {
-            copy_to_lds(pa[t], to + t * WAVES * 1024);
-            pa[t] += kRowBlock;
-        }
+        for (int t = 0; t < PCOPIES; ++t) copy_to_lds(p_base, pa[t], to + t * WAVES * 1024);
 #pragma unroll
-        for (int t = 0; t < QCOPIES; ++t) {
-            copy_to_lds(qa[t], to + PBYTES + t * WAVES * 1024);
-            qa[t] += q_step;
-        }
+        for (int t = 0; t < QCOPIES; ++t) copy_to_lds(q_base, qa[t], to + PBYTES + t * WAVES * 1024);
+        p_base += panel;
+        q_base += q_step;
     };
-    // fragments: row r of 32, values 8 h .. 8 h + 7 of the 16 of step s, plane lo or hi
+    // Fragments of 32 rows by 16 values: lane l holds row l % 32, values 8 (l / 32) .. + 7.  Two of them in a stage, q: hi and
+    // lo, or the two halves of k.
+    struct Frags {
+        half8 p[2][FM], q[2][FN];
+    };
     const int r = lane & 31, h = lane >> 5;
-    auto by_rows = [&](const char *tile, int row, int s, int plane) {
-        const int c = SPLIT ? plane * 4 + s * 2 + h : s * 2 + h;
-        return *reinterpret_cast<const half8 *>(tile + (row + r) * kRowBlock + ((c ^ (((row + r) >> 1) & 7)) * 16));
-    };
-    auto by_columns = [&](const char *tile, int col0, int s, int plane) {
-        union { half8 v; s16x4 part[2]; } u;
+    const int row_at[2] = {r * kRow + ((h ^ ((r >> 2) & 3)) * 16), r * kRow + (((2 + h) ^ ((r >> 2) & 3)) * 16)};
+    int col_at[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int g = (lane >> 4) & 1, k = h * 8 + ((lane & 15) >> 2), byte = (lane & 3) * 8;
+        // split: group g of 16 columns is a panel of its own, hi or lo a half of its rows; one half: a half of the panel's rows
+        col_at[q] = SPLIT ? g * PIECE + k * kRow + ((q ^ g) * 32) + byte : (q * 16 + k) * kRow + g * 32 + byte;
+    }
+    auto read = [&](Frags &f, int buffer) {
+        const char *lp = lds + buffer * STAGE_BYTES + wi * kRow, *lq = lds + buffer * STAGE_BYTES + PBYTES + wj * kRow;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            const int k = s * 16 + h * 8 + q * 4 + ((lane & 15) >> 2), col = col0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-            const int c = SPLIT ? (col >> 5) * 8 + plane * 4 + ((col & 31) >> 3) : col >> 3;
-            const int f = QROW == 128 ? 4 * ((k >> 1) & 1) : 4 * (k & 3);
-            u.part[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + k * QROW + ((c ^ f) * 16) + (col & 7) * 2));
+#pragma unroll
+            for (int b = 0; b < FN; ++b) {
+                if (ACROSS) {
+                    union { half8 v; s16x4 part[2]; } u;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        u.part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lq + b * 32 * kRow + col_at[q] + e * 4 * kRow));
+                    f.q[q][b] = u.v;
+                } else {
+                    f.q[q][b] = *reinterpret_cast<const half8 *>(lq + b * 32 * kRow + row_at[q]);
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < FM; ++a) f.p[q][a] = *reinterpret_cast<const half8 *>(lp + a * 32 * kRow + row_at[q]);
         }
-        return u.v;
     };
     f32x16 acc[FM][FN];
 #pragma unroll
@@ -319,84 +335,138 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
         for (int b = 0; b < FN; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.f;
-    copy(0);
-    for (int k = 0; k < steps_k; ++k) {
-        const int stage = k & 1;
-        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");     // this wavefront's copies into `stage` are there
-        __syncthreads();                                       // everybody's, and nobody reads the other stage any more
-        if (k + 1 < steps_k) copy(1 - stage);
-        const char *lp = lds + stage * STAGE_BYTES, *lq = lp + PBYTES;
-#pragma unroll
-        for (int s = 0; s < KROWS / 16; ++s) {
-            half8 ph[FM], pl[FM], qh[FN], ql[FN];
-#pragma unroll
-            for (int a = 0; a < FM; ++a) {
-                ph[a] = by_rows(lp, wi + a * 32, s, 0);
-                if (SPLIT) pl[a] = by_rows(lp, wi + a * 32, s, 1);
-            }
-#pragma unroll
-            for (int b = 0; b < FN; ++b) {
-                qh[b] = ROWS ? by_columns(lq, wj + b * 32, s, 0) : by_rows(lq, wj + b * 32, s, 0);
-                if (SPLIT) ql[b] = ROWS ? by_columns(lq, wj + b * 32, s, 1) : by_rows(lq, wj + b * 32, s, 1);
-            }
+
+    auto multiply = [&](const Frags &f) {
+        auto one = [&](int qp, int qq) {
 #pragma unroll
             for (int a = 0; a < FM; ++a)
 #pragma unroll
-                for (int b = 0; b < FN; ++b) {
-                    if (SPLIT) {
-                        acc[a][b] = mfma(qh[b], pl[a], acc[a][b]);
-                        acc[a][b] = mfma(ql[b], ph[a], acc[a][b]);
-                    }
-                    acc[a][b] = mfma(qh[b], ph[a], acc[a][b]);
-                }
+                for (int b = 0; b < FN; ++b)
+                    acc[a][b] = mfma(f.q[qq][b], f.p[qp][a], acc[a][b]);
+        };
+        if (SPLIT) {
+            one(1, 0);
+            one(0, 1);
+            one(0, 0);
+        } else {
+            one(0, 0);
+            one(1, 1);
         }
+    };
+    for (int k = 0; k < S && k < stages; ++k) copy(k);
+    Frags f0, f1;
+    if (stages >= S) wait_copies<(S - 1) * COPIES>();
+    else wait_copies<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+    read(f0, 0);
+    int here = 0;                                          // buffer of stage k
+    // Stage k from `now`, stage k + 1 into `next`; steady: as many stages follow as there are buffers.  The last stage
+    // stands by itself, so that on every way to a multiplication the reads of the next fragments come after those of its
+    // own: where the two ways met, the compiler waited for all of them.
+    auto one_stage = [&](auto steady, int k, Frags &now, Frags &next) {
+        const int under_way = stages - 2 - k;              // stages after the next that have been asked for
+        if (decltype(steady)::value || under_way >= S - 2) wait_copies<(S - 2) * COPIES>();
+        else if (S > 3 && under_way == S - 3) wait_copies<(S - 3) * COPIES>();
+        else if (S > 4 && under_way == S - 4) wait_copies<(S - 4) * COPIES>();
+        else wait_copies<0>();
+        // everybody's copies of stage k + 1 are there, and everybody holds stage k in registers
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
+        if (decltype(steady)::value || k + S < stages) copy(here);
+        here = here + 1 == S ? 0 : here + 1;
+        // nothing of this crosses a barrier, and the reads are spread over the first products
+        __builtin_amdgcn_sched_barrier(0);
+        read(next, here);
+        multiply(now);
+#pragma unroll
+        for (int t = 0; t < 2 * (FM + (ACROSS ? 2 : 1) * FN); ++t) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);     // one matrix instruction,
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // one read of LDS
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int k = 0;
+    for (; k + 1 + S < stages; k += 2) {
+        one_stage(std::true_type{}, k, f0, f1);
+        one_stage(std::true_type{}, k + 1, f1, f0);
     }
+    for (; k + 2 < stages; k += 2) {
+        one_stage(std::false_type{}, k, f0, f1);
+        one_stage(std::false_type{}, k + 1, f1, f0);
+    }
+    one_stage(std::false_type{}, k, f0, f1);
+    multiply(f1);
+
     // the product's scale away, the stage's scale on
     const float alpha = STAGE == kGram ? kGramScale / (M.scale * M.scale)
                         : STAGE == kPoly ? step.c * (kPolyScale / (kGramScale * kGramScale)) : 1.0f / kPolyScale;
     const float beta = STAGE == kGram ? 0.f : STAGE == kPoly ? step.b * (kPolyScale / kGramScale) : step.a;
-    const int64_t row_c = ROWS ? M.row_n : M.row_m;
-    const int j_end = ROWS ? M.np : M.mp;
+    const int j_end = ACROSS ? np : mp;
     const char *old = STAGE == kPoly ? P : X;
     char *to = ws + (STAGE == kGram ? M.g : STAGE == kPoly ? M.b : M.x[1 - step.from]);
+    // the last product goes into the vector along its rows, through LDS: a region of its own for every wavefront
+    constexpr int PITCH = WN + 1;
+    float *mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
+    static_assert(WAVES * 32 * PITCH * 4 <= S * STAGE_BYTES, "LDS");
     const float f = M.factor / M.scale;
+    auto into_vector = [&](int i, int j) {
+        if (i0 + wi + i >= M.m || j0 + wj + j >= M.n) return;
+        const int64_t gi = i0 + wi + i, gj = j0 + wj + j, at = M.offset + (M.flip ? gj * M.ld + gi : gi * M.ld + gj);
+        const float o = mine[(i & 31) * PITCH + j] * f;
+        if (OUT == 0) static_cast<float *>(out.dst)[at] = o;
+        else if (OUT == 1) static_cast<uint16_t *>(out.dst)[at] = bf16_round(o);
+        else out.x[at] = __fmaf_rn(-out.gamma, o, out.keep * out.x[at]);
+    };
+    if (STAGE == kLast) __syncthreads();                       // the stages' fragments have been read by everybody
 #pragma unroll
     for (int a = 0; a < FM; ++a) {
-        const int i = i0 + wi + a * 32 + r;
-        if (i0 + wi + a * 32 >= M.mp) break;                   // rounded sizes are multiples of 64: whole 32 x 32 parts
+        const int ib = i0 + wi + a * 32;
+        if (ib >= mp) break;                                   // rounded sizes are multiples of 64: whole 32 x 32 parts
 #pragma unroll
         for (int b = 0; b < FN; ++b) {
             const int jb = j0 + wj + b * 32;
             if (jb >= j_end) break;
+            // lane: row r, columns 8 g + 4 h + e; the two halves of the wavefront exchange, so that a lane has eight in a row
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int j = jb + 8 * g + 4 * h;
-                const int64_t at = chunk_at<SPLIT>(row_c, i, j);
-                float v[4];
-                if (STAGE != kGram) load4<SPLIT>(old + at, v);
+            for (int g = 0; g < 2; ++g) {
+                float v[8], x[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = acc[a][b][4 * g + e] * alpha;
-                    v[e] = STAGE == kGram ? p : __fmaf_rn(beta, v[e], p);
+                    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[a][b][8 * g + e]),
+                                                                    __float_as_uint(acc[a][b][8 * g + 4 + e]), false, false);
+                    v[e] = __uint_as_float(w[0]);
+                    v[4 + e] = __uint_as_float(w[1]);
                 }
+                const int i = ib + r, j = jb + 16 * g + 8 * h;
+                const int64_t at = element_at<SPLIT>(panel, i, j);
+                if (STAGE != kGram) load8<SPLIT>(old + at, x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = STAGE == kGram ? v[e] * alpha : __fmaf_rn(beta, x[e], v[e] * alpha);
                 if constexpr (STAGE != kLast) {
-                    store4<SPLIT>(to + at, v);
+                    store8<SPLIT>(to + at, v);
                     if (STAGE < kApply && tl.i != tl.j) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) store1<SPLIT>(to + chunk_at<SPLIT>(row_c, j + e, i & ~7) + (i & 7) * 2, v[e]);
+                        for (int e = 0; e < 8; ++e) store1<SPLIT>(to + element_at<SPLIT>(panel, j + e, i), v[e]);
                     }
-                } else if (i < M.m) {
+                } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (j + e >= M.n) break;
-                        const int64_t o_at = M.offset + (M.flip ? (j + e) * M.ld + i : i * M.ld + j + e);
-                        const float o = v[e] * f;
-                        if (OUT == 0) static_cast<float *>(out.dst)[o_at] = o;
-                        else if (OUT == 1) static_cast<uint16_t *>(out.dst)[o_at] = bf16_round(o);
-                        else out.x[o_at] = __fmaf_rn(-out.gamma, o, out.keep * out.x[o_at]);
-                    }
+                    for (int e = 0; e < 8; ++e) mine[r * PITCH + b * 32 + 16 * g + 8 * h + e] = v[e];
                 }
             }
+        }
+        if constexpr (STAGE == kLast) {
+            // written and read by the same wavefront: its own accesses of LDS stay in order
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+            constexpr int PER = 64 / WN;                       // rows that 64 lanes write at a time
+            if (M.flip) {
+#pragma unroll 8
+                for (int t = 0; t < 32 * WN / 64; ++t) into_vector(a * 32 + r, 2 * t + h);
+            } else {
+#pragma unroll 8
+                for (int t = 0; t < 32 / PER; ++t) into_vector(a * 32 + t * PER + lane / WN, lane % WN);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
         }
     }
 }
@@ -521,8 +591,7 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
         M.n = std::max(in.rows, in.cols);
         M.mp = static_cast<int32_t>(round_up(M.m, kTileSide));
         M.np = static_cast<int32_t>(round_up(M.n, kTileSide));
-        M.row_n = M.np * (split ? 4 : 2);
-        M.row_m = M.mp * (split ? 4 : 2);
+        M.panel = M.mp * kRow;
         // entries of an orthogonal [m, n] matrix are about 1 / sqrt(n); 16 there leaves 2^-25 of an entry to lo, and
         // 2^14 keeps the largest possible one, singular value 2, below the largest half
         int s = 4;
@@ -536,10 +605,11 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
             t.ws_bytes += round_up(bytes, 256);
             return at;
         };
-        M.x[0] = take(static_cast<int64_t>(M.mp) * M.row_n);
-        M.x[1] = take(static_cast<int64_t>(M.mp) * M.row_n);
-        M.g = take(static_cast<int64_t>(M.mp) * M.row_m);
-        M.b = take(static_cast<int64_t>(M.mp) * M.row_m);
+        const int64_t each = split ? 4 : 2;
+        M.x[0] = take(static_cast<int64_t>(M.mp) * M.np * each);
+        M.x[1] = take(static_cast<int64_t>(M.mp) * M.np * each);
+        M.g = take(static_cast<int64_t>(M.mp) * M.mp * each);
+        M.b = take(static_cast<int64_t>(M.mp) * M.mp * each);
         const int64_t elements = static_cast<int64_t>(M.m) * M.n;
         M.parts = static_cast<int32_t>(std::min<int64_t>(kMaxParts, (elements + kPartElements - 1) / kPartElements));
         M.part0 = static_cast<int32_t>(t.n_partial);
@@ -561,9 +631,9 @@ void product(const ds_ortho *o, const Step &s, const Out &out, hipStream_t st)
     const Tile *tiles = WIDE ? o->wide : o->square;
     const unsigned n = static_cast<unsigned>(WIDE ? o->n_wide : o->n_square);
     switch (WIDE ? o->wide_side : o->square_side) {
-    case 256: k_ortho_product<256, 256, 128, 64, SPLIT, STAGE, OUT><<<n, 512, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
-    case 128: k_ortho_product<128, 128, 64, 64, SPLIT, STAGE, OUT><<<n, 256, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
-    default: k_ortho_product<64, 64, 32, 32, SPLIT, STAGE, OUT><<<n, 256, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
+    case 256: k_ortho_product<256, 256, 128, 64, 4, SPLIT, STAGE, OUT><<<n, 512, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
+    case 128: k_ortho_product<128, 128, 64, 64, 4, SPLIT, STAGE, OUT><<<n, 256, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
+    default: k_ortho_product<64, 64, 32, 32, 4, SPLIT, STAGE, OUT><<<n, 256, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
     }
 }
 
