@@ -42,7 +42,7 @@ constexpr int kRow = 64;                       // bytes of a row in a panel
 constexpr float kGramScale = 8192.0f;          // G is held times 2^13 (entries up to 8)
 constexpr float kPolyScale = 4096.0f;          // B is held times 2^12 (entries up to 16)
 constexpr int kTileSide = 64;
-constexpr int kMaxParts = 256;                 // partial sums of a matrix's norm
+constexpr int kMaxParts = 512;                 // partial sums of a matrix's norm
 constexpr int64_t kPartElements = 16384;
 
 struct Mat {
@@ -124,7 +124,16 @@ __device__ __forceinline__ uint16_t bf16_round(float x)      // to nearest, ties
 // ---------------------------------------------------------------------------------------
 // norms and operands
 // ---------------------------------------------------------------------------------------
-// Partial sums of squares in fp64: part p of a matrix is a run of its rows' elements.
+// Four elements from `at` on, zero past `lim`; any alignment.
+template <bool BF16>
+__device__ __forceinline__ f32x4 load_flat4(const void *p, int64_t at, int64_t lim)
+{
+    if (!BF16) return ld4(static_cast<const float *>(p), at, lim);
+    return ld4_bf16(static_cast<const uint16_t *>(p), at, lim);
+}
+
+// Partial sums of squares in fp64: part p of a matrix is a run of its elements.  Bound by the reads of U (sixty matrices, 85 M
+// elements: 340 MB).
 template <bool BF16>
 __global__ __launch_bounds__(kBlock) void k_ortho_norm(const Mat *__restrict__ mats, const int2 *__restrict__ parts, const void *src,
                                                        double *__restrict__ partial)
@@ -136,10 +145,22 @@ __global__ __launch_bounds__(kBlock) void k_ortho_norm(const Mat *__restrict__ m
     const int64_t each = ((total + M.parts - 1) / M.parts + 3) & ~static_cast<int64_t>(3);
     const int64_t lo = each * pt.y, hi = lo + each < total ? lo + each : total;
     double s = 0.0;
-    for (int64_t t = lo + threadIdx.x; t < hi; t += kBlock) {
-        const uint32_t r = static_cast<uint32_t>(t) / static_cast<uint32_t>(M.cols);
-        const double v = load_flat<BF16>(src, M.offset + r * M.ld + (t - static_cast<int64_t>(r) * M.cols));
-        s += v * v;
+    if (M.ld == M.cols) {
+#pragma unroll 8
+        for (int64_t t = lo + threadIdx.x * 4; t < hi; t += kBlock * 4) {
+            const f32x4 v = load_flat4<BF16>(src, M.offset + t, M.offset + hi);
+            const double a = v.x, b = v.y, c = v.z, d = v.w;
+            s = fma(a, a, s);
+            s = fma(b, b, s);
+            s = fma(c, c, s);
+            s = fma(d, d, s);
+        }
+    } else {
+        for (int64_t t = lo + threadIdx.x; t < hi; t += kBlock) {
+            const uint32_t r = static_cast<uint32_t>(t) / static_cast<uint32_t>(M.cols);
+            const double v = load_flat<BF16>(src, M.offset + r * M.ld + (t - static_cast<int64_t>(r) * M.cols));
+            s = fma(v, v, s);
+        }
     }
     s = block_sum(s, lds, false);
     if (threadIdx.x == 0) partial[M.part0 + pt.y] = s;
@@ -155,6 +176,17 @@ __global__ __launch_bounds__(kThreads) void k_ortho_operands(const Mat *__restri
     __shared__ double sums[kThreads / 64];
     const Tile tl = tiles[blockIdx.x];
     const Mat &M = mats[tl.mat];
+    const int i0 = tl.i * T, j0 = tl.j * T;
+    // the stored rows: four elements of one a thread, four rows
+    const int row0 = M.flip ? j0 : i0, col0 = M.flip ? i0 : j0;
+    const int c4 = (threadIdx.x & 15) * 4, r4 = threadIdx.x >> 4;
+    f32x4 v[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int rr = row0 + r4 + 16 * t, c = col0 + c4;
+        const int64_t row = M.offset + static_cast<int64_t>(rr) * M.ld;
+        v[t] = rr < M.rows && c < M.cols ? load_flat4<BF16>(src, row + c, row + M.cols) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     double s = 0.0;
     for (int p = threadIdx.x; p < M.parts; p += kThreads) s += partial[M.part0 + p];
     s = wave_sum(s);
@@ -165,17 +197,13 @@ __global__ __launch_bounds__(kThreads) void k_ortho_operands(const Mat *__restri
     for (int w = 0; w < kThreads / 64; ++w) s += sums[w];
     const double norm = sqrt(s) + static_cast<double>(eps);
     const double inv = norm == 0.0 ? 0.0 : static_cast<double>(M.scale) / norm;
-    const int i0 = tl.i * T, j0 = tl.j * T;
-    for (int t = threadIdx.x; t < T * T; t += kThreads) {
-        const int fast = t & (T - 1), slow = t / T;
-        const int i = M.flip ? fast : slow, j = M.flip ? slow : fast;
-        float v = 0.f;
-        if (i0 + i < M.m && j0 + j < M.n) {
-            const int64_t r = M.flip ? j0 + j : i0 + i, c = M.flip ? i0 + i : j0 + j;
-            v = static_cast<float>(static_cast<double>(load_flat<BF16>(src, M.offset + r * M.ld + c)) * inv);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int rr = r4 + 16 * t, c = c4 + e;
+            (M.flip ? tile[c][rr] : tile[rr][c]) = static_cast<float>(static_cast<double>(v[t][e]) * inv);
         }
-        tile[i][j] = v;
-    }
     __syncthreads();
     for (int t = threadIdx.x; t < T * T / 8; t += kThreads) {
         const int a = t / (T / 8), c = (t % (T / 8)) * 8;
@@ -410,19 +438,33 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     float *mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
     static_assert(WAVES * 32 * PITCH * 4 <= S * STAGE_BYTES, "LDS");
     const float f = M.factor / M.scale;
-    auto into_vector = [&](int i, int j) {
-        if (i0 + wi + i >= M.m || j0 + wj + j >= M.n) return;
-        const int64_t gi = i0 + wi + i, gj = j0 + wj + j, at = M.offset + (M.flip ? gj * M.ld + gi : gi * M.ld + gj);
-        const float o = mine[(i & 31) * PITCH + j] * f;
-        if (OUT == 0) static_cast<float *>(out.dst)[at] = o;
-        else if (OUT == 1) static_cast<uint16_t *>(out.dst)[at] = bf16_round(o);
-        else out.x[at] = __fmaf_rn(-out.gamma, o, out.keep * out.x[at]);
+    // element t of the 32 rows of part a that this lane writes: 64 lanes along the rows of the vector
+    constexpr int EACH = 32 * WN / 64;
+    auto place = [&](int a, int t, int &i, int &j) {
+        if (M.flip) {
+            i = r;
+            j = 2 * t + h;
+        } else {
+            i = t * (64 / WN) + lane / WN;
+            j = lane % WN;
+        }
+        const int64_t gi = i0 + wi + a * 32 + i, gj = j0 + wj + j;
+        return gi < M.m && gj < M.n ? M.offset + (M.flip ? gj * M.ld + gi : gi * M.ld + gj) : static_cast<int64_t>(-1);
     };
     if (STAGE == kLast) __syncthreads();                       // the stages' fragments have been read by everybody
 #pragma unroll
     for (int a = 0; a < FM; ++a) {
         const int ib = i0 + wi + a * 32;
         if (ib >= mp) break;                                   // rounded sizes are multiples of 64: whole 32 x 32 parts
+        float model[STAGE == kLast && OUT == 2 ? EACH : 1];
+        if constexpr (STAGE == kLast && OUT == 2) {            // asked for early: they arrive while the part is put together
+#pragma unroll
+            for (int t = 0; t < EACH; ++t) {
+                int i, j;
+                const int64_t at = place(a, t, i, j);
+                model[t] = at >= 0 ? __builtin_nontemporal_load(out.x + at) : 0.f;
+            }
+        }
 #pragma unroll
         for (int b = 0; b < FN; ++b) {
             const int jb = j0 + wj + b * 32;
@@ -458,13 +500,15 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
         if constexpr (STAGE == kLast) {
             // written and read by the same wavefront: its own accesses of LDS stay in order
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-            constexpr int PER = 64 / WN;                       // rows that 64 lanes write at a time
-            if (M.flip) {
-#pragma unroll 8
-                for (int t = 0; t < 32 * WN / 64; ++t) into_vector(a * 32 + r, 2 * t + h);
-            } else {
-#pragma unroll 8
-                for (int t = 0; t < 32 / PER; ++t) into_vector(a * 32 + t * PER + lane / WN, lane % WN);
+#pragma unroll
+            for (int t = 0; t < EACH; ++t) {
+                int i, j;
+                const int64_t at = place(a, t, i, j);
+                if (at < 0) continue;
+                const float o = mine[i * PITCH + j] * f;
+                if (OUT == 0) __builtin_nontemporal_store(o, static_cast<float *>(out.dst) + at);
+                else if (OUT == 1) __builtin_nontemporal_store(bf16_round(o), static_cast<uint16_t *>(out.dst) + at);
+                else __builtin_nontemporal_store(__fmaf_rn(-out.gamma, o, out.keep * model[t]), out.x + at);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
         }
