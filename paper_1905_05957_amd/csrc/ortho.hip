@@ -57,8 +57,14 @@ struct Mat {
     float factor;
 };
 
+// What a workgroup of a product takes: tile (i, j) of a matrix, stages [k0, k1) of its sum.  slot < 0: the whole sum; else this
+// part goes to that slot of the parts' buffer and a launch behind the product puts the parts together.
 struct Tile {
-    int32_t mat, i, j, pad_;
+    int32_t mat, i, j, k0, k1, slot, pad_[2];
+};
+
+struct Cut {                     // a tile in parts
+    int32_t mat, i, j, slot, n, pad_[3];
 };
 
 template <bool SPLIT>
@@ -119,6 +125,22 @@ __device__ __forceinline__ uint16_t bf16_round(float x)      // to nearest, ties
     const uint32_t u = __float_as_uint(x);
     if ((u & 0x7FFFFFFFu) > 0x7F800000u) return static_cast<uint16_t>((u >> 16) | 0x40u);
     return static_cast<uint16_t>((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
+}
+
+// Eight elements, the first n of them.
+__device__ __forceinline__ void store_bf16(uint16_t *p, int n, const float *v)
+{
+    typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+    if (n >= 8) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = bf16_round(v[2 * e]) | (static_cast<uint32_t>(bf16_round(v[2 * e + 1])) << 16);
+        __builtin_nontemporal_store(static_cast<u32x4_any>(w), reinterpret_cast<u32x4_any *>(p));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < n) p[e] = bf16_round(v[e]);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -252,6 +274,35 @@ __device__ __forceinline__ f32x16 mfma(half8 a, half8 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+// Factors of the product and of the old value: the operands' scales away, the result's scale on.
+template <int STAGE>
+__device__ __forceinline__ float product_scale(const Mat &M, const Step &step)
+{
+    return STAGE == kGram ? kGramScale / (M.scale * M.scale)
+           : STAGE == kPoly ? step.c * (kPolyScale / (kGramScale * kGramScale)) : 1.0f / kPolyScale;
+}
+
+template <int STAGE>
+__device__ __forceinline__ float old_scale(const Step &step)
+{
+    return STAGE == kGram ? 0.f : STAGE == kPoly ? step.b * (kPolyScale / kGramScale) : step.a;
+}
+
+// Of a 32 x 32 part a lane holds row l % 32 and columns 8 t + 4 (l / 32) .. + 3, t = 0 .. 3; here the wavefront's halves
+// exchange, and the lane has the eight columns from 16 g + 8 (l / 32) on.
+struct EightColumns {
+    float v[8];
+    __device__ __forceinline__ EightColumns(const f32x16 &acc, int g)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[8 * g + e]), __float_as_uint(acc[8 * g + 4 + e]), false, false);
+            v[e] = __uint_as_float(w[0]);
+            v[4 + e] = __uint_as_float(w[1]);
+        }
+    }
+};
+
 template <int N>
 __device__ __forceinline__ void wait_copies()       // at most N copies of this wavefront under way, and its reads of LDS are done
 {
@@ -272,7 +323,7 @@ __device__ __forceinline__ void wait_copies()       // at most N copies of this 
 // The wavefront multiplies Q' P': a lane then holds a row i of C and four consecutive j at a time.
 template <int TM, int TN, int WM, int WN, int S, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
 __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Mat *__restrict__ mats, const Tile *__restrict__ tiles,
-                                                                             char *ws, Step step, Out out)
+                                                                             char *ws, float *parts, Step step, Out out)
 {
     constexpr int WAVES_N = TN / WN, WAVES = (TM / WM) * WAVES_N, FM = WM / 32, FN = WN / 32;
     constexpr bool ACROSS = STAGE >= kApply;                   // Q is X
@@ -287,7 +338,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int wi = (wave / WAVES_N) * WM, wj = (wave % WAVES_N) * WN;
     const int64_t panel = M.panel;
-    const int stages = (STAGE == kGram ? np : mp) / K;         // even: rounded sizes are multiples of 64
+    const int stages = tl.k1 - tl.k0;                          // even: rounded sizes are multiples of 64
     const char *X = ws + M.x[step.from];
     const char *P = STAGE == kGram ? X : ws + (STAGE == kPoly ? M.g : M.b);
     const char *Q = ACROSS ? X : P;
@@ -312,6 +363,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
         }
     }
     const int64_t q_step = ACROSS ? PIECE : panel;
+    p_base += tl.k0 * panel;
+    q_base += tl.k0 * q_step;
     const uint32_t lds_at = __builtin_amdgcn_readfirstlane(lds_address(lds)) + wave * 1024;
     auto copy = [&](int buffer) {
         const uint32_t to = lds_at + buffer * STAGE_BYTES;
@@ -426,10 +479,23 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     one_stage(std::false_type{}, k, f0, f1);
     multiply(f1);
 
-    // the product's scale away, the stage's scale on
-    const float alpha = STAGE == kGram ? kGramScale / (M.scale * M.scale)
-                        : STAGE == kPoly ? step.c * (kPolyScale / (kGramScale * kGramScale)) : 1.0f / kPolyScale;
-    const float beta = STAGE == kGram ? 0.f : STAGE == kPoly ? step.b * (kPolyScale / kGramScale) : step.a;
+    if (tl.slot >= 0) {
+        // eight columns of all rows behind each other: what 64 threads of the joining launch read lies together
+        float *mine = parts + static_cast<int64_t>(tl.slot) * (TM * TN);
+#pragma unroll
+        for (int a = 0; a < FM; ++a)
+#pragma unroll
+            for (int b = 0; b < FN; ++b)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const EightColumns c(acc[a][b], g);
+                    float *p = mine + (((wj + b * 32 + 16 * g) / 8 + h) * TM + wi + a * 32 + r) * 8;
+                    *reinterpret_cast<f32x4 *>(p) = f32x4{c.v[0], c.v[1], c.v[2], c.v[3]};
+                    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{c.v[4], c.v[5], c.v[6], c.v[7]};
+                }
+        return;
+    }
+    const float alpha = product_scale<STAGE>(M, step), beta = old_scale<STAGE>(step);
     const int j_end = ACROSS ? np : mp;
     const char *old = STAGE == kPoly ? P : X;
     char *to = ws + (STAGE == kGram ? M.g : STAGE == kPoly ? M.b : M.x[1 - step.from]);
@@ -438,53 +504,47 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     float *mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
     static_assert(WAVES * 32 * PITCH * 4 <= S * STAGE_BYTES, "LDS");
     const float f = M.factor / M.scale;
-    // element t of the 32 rows of part a that this lane writes: 64 lanes along the rows of the vector
-    constexpr int EACH = 32 * WN / 64;
-    auto place = [&](int a, int t, int &i, int &j) {
+    // Vector t of the 32 rows of part a that this lane writes: V elements along a row of the vector.
+    constexpr int V = OUT == 1 ? 8 : 4, EACH = 32 * WN / (64 * V);
+    auto place = [&](int a, int t, int &i, int &j, int &n) {   // its first element in the part, and how many there are
         if (M.flip) {
-            i = r;
-            j = 2 * t + h;
+            i = (lane % (32 / V)) * V;
+            j = t * (64 * V / 32) + lane / (32 / V);
         } else {
-            i = t * (64 / WN) + lane / WN;
-            j = lane % WN;
+            i = t * (64 * V / WN) + lane / (WN / V);
+            j = (lane % (WN / V)) * V;
         }
         const int64_t gi = i0 + wi + a * 32 + i, gj = j0 + wj + j;
-        return gi < M.m && gj < M.n ? M.offset + (M.flip ? gj * M.ld + gi : gi * M.ld + gj) : static_cast<int64_t>(-1);
+        n = M.flip ? (gj < M.n ? M.m - static_cast<int>(gi) : 0) : (gi < M.m ? M.n - static_cast<int>(gj) : 0);
+        return M.offset + (M.flip ? gj * M.ld + gi : gi * M.ld + gj);
     };
     if (STAGE == kLast) __syncthreads();                       // the stages' fragments have been read by everybody
 #pragma unroll
     for (int a = 0; a < FM; ++a) {
         const int ib = i0 + wi + a * 32;
         if (ib >= mp) break;                                   // rounded sizes are multiples of 64: whole 32 x 32 parts
-        float model[STAGE == kLast && OUT == 2 ? EACH : 1];
+        f32x4 model[STAGE == kLast && OUT == 2 ? EACH : 1];
         if constexpr (STAGE == kLast && OUT == 2) {            // asked for early: they arrive while the part is put together
 #pragma unroll
             for (int t = 0; t < EACH; ++t) {
-                int i, j;
-                const int64_t at = place(a, t, i, j);
-                model[t] = at >= 0 ? __builtin_nontemporal_load(out.x + at) : 0.f;
+                int i, j, n;
+                const int64_t at = place(a, t, i, j, n);
+                model[t] = n > 0 ? ld4_stream(out.x, at, at + n) : f32x4{0.f, 0.f, 0.f, 0.f};
             }
         }
 #pragma unroll
         for (int b = 0; b < FN; ++b) {
             const int jb = j0 + wj + b * 32;
             if (jb >= j_end) break;
-            // lane: row r, columns 8 g + 4 h + e; the two halves of the wavefront exchange, so that a lane has eight in a row
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
+                const EightColumns c(acc[a][b], g);
                 float v[8], x[8];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[a][b][8 * g + e]),
-                                                                    __float_as_uint(acc[a][b][8 * g + 4 + e]), false, false);
-                    v[e] = __uint_as_float(w[0]);
-                    v[4 + e] = __uint_as_float(w[1]);
-                }
                 const int i = ib + r, j = jb + 16 * g + 8 * h;
                 const int64_t at = element_at<SPLIT>(panel, i, j);
                 if (STAGE != kGram) load8<SPLIT>(old + at, x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = STAGE == kGram ? v[e] * alpha : __fmaf_rn(beta, x[e], v[e] * alpha);
+                for (int e = 0; e < 8; ++e) v[e] = STAGE == kGram ? c.v[e] * alpha : __fmaf_rn(beta, x[e], c.v[e] * alpha);
                 if constexpr (STAGE != kLast) {
                     store8<SPLIT>(to + at, v);
                     if (STAGE < kApply && tl.i != tl.j) {
@@ -502,15 +562,68 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
 #pragma unroll
             for (int t = 0; t < EACH; ++t) {
-                int i, j;
-                const int64_t at = place(a, t, i, j);
-                if (at < 0) continue;
-                const float o = mine[i * PITCH + j] * f;
-                if (OUT == 0) __builtin_nontemporal_store(o, static_cast<float *>(out.dst) + at);
-                else if (OUT == 1) __builtin_nontemporal_store(bf16_round(o), static_cast<uint16_t *>(out.dst) + at);
-                else __builtin_nontemporal_store(__fmaf_rn(-out.gamma, o, out.keep * model[t]), out.x + at);
+                int i, j, n;
+                const int64_t at = place(a, t, i, j, n);
+                if (n <= 0) continue;
+                float o[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) o[e] = mine[M.flip ? (i + e) * PITCH + j : i * PITCH + j + e] * f;
+                if constexpr (OUT == 1) {
+                    store_bf16(static_cast<uint16_t *>(out.dst) + at, n, o);
+                } else {
+                    f32x4 v = {o[0], o[1], o[2], o[3]};
+                    if (OUT == 2) v = fma4(-out.gamma, v, out.keep * model[t]);
+                    st4_stream(OUT == 2 ? out.x : static_cast<float *>(out.dst), at, at + n, v);
+                }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        }
+    }
+}
+
+// Tiles whose sums were taken in parts: the parts in their order, then as a whole tile goes on.  A thread takes eight columns of
+// a row, a wavefront 64 rows.
+template <int SIDE, bool SPLIT, int STAGE, int OUT>
+__global__ __launch_bounds__(kThreads) void k_ortho_join(const Mat *__restrict__ mats, const Cut *__restrict__ cuts, char *ws,
+                                                         const float *__restrict__ parts, Step step, Out out)
+{
+    constexpr int PER_TILE = SIDE * SIDE / 8 / kThreads;
+    const Cut cut = cuts[blockIdx.x / PER_TILE];
+    const Mat &M = mats[cut.mat];
+    const int t = (blockIdx.x % PER_TILE) * kThreads + threadIdx.x, row = t % SIDE, col = t / SIDE * 8;
+    const int i = cut.i * SIDE + row, j = cut.j * SIDE + col;
+    if (i >= M.mp || j >= (STAGE >= kApply ? M.np : M.mp)) return;
+    const float *from = parts + static_cast<int64_t>(cut.slot) * (SIDE * SIDE) + t * 8;
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll 4
+    for (int p = 0; p < cut.n; ++p) {
+        s0 += *reinterpret_cast<const f32x4 *>(from);
+        s1 += *reinterpret_cast<const f32x4 *>(from + 4);
+        from += SIDE * SIDE;
+    }
+    const float alpha = product_scale<STAGE>(M, step), beta = old_scale<STAGE>(step);
+    const int64_t at = element_at<SPLIT>(M.panel, i, j);
+    float v[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w}, x[8];
+    if (STAGE != kGram) load8<SPLIT>(ws + (STAGE == kPoly ? M.g : M.x[step.from]) + at, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = STAGE == kGram ? v[e] * alpha : __fmaf_rn(beta, x[e], v[e] * alpha);
+    if constexpr (STAGE != kLast) {
+        char *to = ws + (STAGE == kGram ? M.g : STAGE == kPoly ? M.b : M.x[1 - step.from]);
+        store8<SPLIT>(to + at, v);
+        if (STAGE < kApply && cut.i != cut.j) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) store1<SPLIT>(to + element_at<SPLIT>(M.panel, j + e, i), v[e]);
+        }
+    } else if (i < M.m) {
+        const float f = M.factor / M.scale;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (j + e >= M.n) break;
+            const int64_t to = M.offset + (M.flip ? static_cast<int64_t>(j + e) * M.ld + i : static_cast<int64_t>(i) * M.ld + j + e);
+            const float o = v[e] * f;
+            if (OUT == 0) static_cast<float *>(out.dst)[to] = o;
+            else if (OUT == 1) static_cast<uint16_t *>(out.dst)[to] = bf16_round(o);
+            else out.x[to] = __fmaf_rn(-out.gamma, o, out.keep * out.x[to]);
         }
     }
 }
@@ -526,10 +639,17 @@ struct ds_ortho {
     std::vector<float> coef;
     void *mem;                             // one allocation behind everything below
     const Mat *mats;
-    const Tile *square, *wide, *operands;  // tiles of G and B, of X, and of the operands' pass
+    struct Launch {                        // a product of all matrices
+        const Tile *tiles;
+        const Cut *cuts;
+        unsigned n_tiles, n_cuts;
+        int side;
+    };
+    Launch gram, poly, wide;               // X X' ; G G ; B X
+    const Tile *operands;
     const int2 *parts;
-    int64_t n_square, n_wide, n_operands, n_parts;
-    int square_side, wide_side;
+    int64_t n_operands, n_parts;
+    float *sums;                           // parts of sums
     double *partial;
     uint64_t *inside;                      // plane of bits: the elements of the matrices
     float *u;                              // [d] what is orthogonalised, where it is not m
@@ -554,71 +674,161 @@ bool mark(std::vector<uint64_t> &plane, int64_t lo, int64_t hi)
     return true;
 }
 
+// The tiles of a product in the order in which they are given out.
+struct Work {
+    std::vector<Tile> tiles;
+    std::vector<Cut> cuts;
+    int32_t slots = 0;                     // of the parts' buffer
+    int side = 64;
+};
+
 // Tables of the plan; the matrices were checked.
 struct Tables {
     std::vector<Mat> mats;
-    std::vector<Tile> square, wide, operands;
+    Work gram, poly, wide;
+    std::vector<Tile> operands;
     std::vector<int2> parts;
     int64_t n_partial = 0, ws_bytes = 0;
-    int square_side = 64, wide_side = 64;
 };
 
-// Tiles of `side` in the order in which they are given out: long sums first, so that the launch ends with short ones; within a
-// matrix strips of rows, so that tiles near each other in time share rows and columns; runs of kRun tiles to one XCD
-// (workgroup p runs on XCD p % 8, each with an L2 of its own).
-std::vector<Tile> make_tiles(const std::vector<Mat> &mats, int side, bool square)
+// All tiles of a product: long sums first, so that the launch ends with short ones; within a matrix strips of rows, so that
+// tiles near each other in time share rows and columns.
+std::vector<Tile> list_tiles(const std::vector<Mat> &mats, int side, int stage, int panel)
 {
-    constexpr size_t kRun = 32;
     std::vector<int32_t> order(mats.size());
     for (size_t k = 0; k < mats.size(); ++k) order[k] = static_cast<int32_t>(k);
-    auto length = [&](int32_t k) { return square ? mats[k].np : mats[k].mp; };
+    auto length = [&](int32_t k) { return stage == kGram ? mats[k].np : mats[k].mp; };
     std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return length(a) > length(b); });
     std::vector<Tile> list;
     const int32_t strip = 1024 / side;
+    const bool square = stage != kApply;
     for (int32_t k : order) {
         const int32_t ti = (mats[k].mp + side - 1) / side, tj = square ? ti : (mats[k].np + side - 1) / side;
         for (int32_t i0 = 0; i0 < ti; i0 += strip)
             for (int32_t j = 0; j < tj; ++j)
                 for (int32_t i = i0; i < std::min(i0 + strip, ti); ++i)
-                    if (!square || j <= i) list.push_back(Tile{k, i, j, 0});
+                    if (!square || j <= i) list.push_back(Tile{k, i, j, 0, length(k) / panel, -1, {0, 0}});
     }
+    return list;
+}
+
+// Runs of kRun tiles to one XCD (workgroup p runs on XCD p % 8, each with an L2 of its own).
+std::vector<Tile> by_xcd(const std::vector<Tile> &list)
+{
+    constexpr size_t kRun = 32;
     std::vector<Tile> out;
     out.reserve(list.size());
     size_t next[8], xcd = 0;
     for (size_t q = 0; q < 8; ++q) next[q] = q * kRun;
     while (out.size() < list.size()) {
-        if (next[xcd] < list.size()) {
-            out.push_back(list[next[xcd]]);
-            if (++next[xcd] % kRun == 0) next[xcd] += 7 * kRun;
-        } else {
+        size_t from = xcd;
+        if (next[from] >= list.size()) {
             // nothing is left for this XCD: its turn goes to the one that has most left
-            size_t far = 8;
+            from = 8;
             for (size_t q = 0; q < 8; ++q)
-                if (next[q] < list.size() && (far == 8 || next[q] < next[far])) far = q;
-            out.push_back(list[next[far]]);
-            if (++next[far] % kRun == 0) next[far] += 7 * kRun;
+                if (next[q] < list.size() && (from == 8 || next[q] < next[from])) from = q;
         }
+        out.push_back(list[next[from]]);
+        if (++next[from] % kRun == 0) next[from] += 7 * kRun;
         xcd = (xcd + 1) % 8;
     }
     return out;
 }
 
-int64_t count_tiles(const std::vector<Mat> &mats, int side, bool square)
+// What a launch of these tiles takes, in microseconds, from times measured with 1 to 4096 tiles of 16 to 512 stages.  A
+// workgroup takes `base` (addresses, first copies, results) and a time per stage, which grow with the workgroups per
+// compute unit (c): alone and with the device full a stage of a 256 x 256 tile takes 0.75 and 1.25 us (0.55 and 0.95 with one half; 32 values of k then), of a 128 x 128
+// tile 0.25 and, two per compute unit, 0.68 (0.19, 0.53), of a 64 x 64 tile 0.16 and, four, 0.48 (0.13, 0.45).
+double launch_time(const std::vector<Tile> &tiles, int side, bool split)
 {
-    int64_t n = 0;
-    for (const Mat &M : mats) {
-        const int64_t ti = (M.mp + side - 1) / side, tj = (M.np + side - 1) / side;
-        n += square ? ti * (ti + 1) / 2 : ti * tj;
+    const size_t at_once = side == 256 ? 256 : side == 128 ? 512 : 1024;
+    double time = 0.0;
+    for (size_t first = 0; first < tiles.size(); first += at_once) {
+        const size_t end = std::min(first + at_once, tiles.size());
+        const double c = static_cast<double>(end - first) / 256.0;
+        int64_t longest = 0, sum = 0;
+        for (size_t k = first; k < end; ++k) {
+            longest = std::max<int64_t>(longest, tiles[k].k1 - tiles[k].k0);
+            sum += tiles[k].k1 - tiles[k].k0;
+        }
+        const double stage = side == 256 ? (split ? 0.75 + 0.5 * c : 0.55 + 0.4 * c)
+                             : side == 128 ? (c <= 1.0 ? 0.06 * c + (split ? 0.25 : 0.19) : (split ? 0.31 + 0.37 * (c - 1.0) : 0.25 + 0.28 * (c - 1.0)))
+                                           : 0.08 * c + (split ? 0.16 : 0.13);
+        const double more = std::max(c - 1.0, 0.0);
+        const double base = side == 256 ? (split ? 13.0 : 7.0) : side == 128 ? 4.5 + (split ? 7.5 : 3.5) * more : 2.2 + (split ? 1.2 : 0.3) * more;
+        // rounds run into each other: only the last one's longest sum counts in full
+        time += base + stage * (end == tiles.size() ? static_cast<double>(longest) : static_cast<double>(sum) / static_cast<double>(end - first));
     }
-    return n;
+    return time;
 }
 
-// Side of the tiles: rounds of the device's 256 compute units times the time of a tile.
-int tile_side(const std::vector<Mat> &mats, bool square)
+// A product by tiles of `side`.  The device takes `at_once` workgroups; a workgroup's share of all stages is what it would have
+// if they were dealt out evenly.  Tiles that fit into the shares stay whole; the others (those of a last round that would
+// leave most of the device idle, or sums longer than a share) are cut into parts that do, if `cutting`.
+void deal_out(const std::vector<Tile> &list, int side, bool cutting, Work &w)
 {
-    auto rounds = [&](int side, int64_t at_once) { return static_cast<double>((count_tiles(mats, side, square) + at_once - 1) / at_once); };
-    const double t256 = rounds(256, 256) * 1.0, t128 = rounds(128, 512) * 0.55, t64 = rounds(64, 1024) * 0.35;
-    return t64 < t128 && t64 < t256 ? 64 : t128 < t256 ? 128 : 256;
+    constexpr int kLeast = 8;              // stages of a part: below, filling the pipeline costs more than it saves
+    const int at_once = side == 256 ? 256 : side == 128 ? 512 : 1024;
+    w.side = side;
+    std::vector<Tile> whole, cut, pieces;
+    int64_t total = 0, cut_stages = 0;
+    for (const Tile &t : list) total += t.k1;
+    const int64_t share = std::max<int64_t>((total + at_once - 1) / at_once, kLeast);
+    // the launch as the device would deal it out: every tile to the workgroup that is free first
+    std::vector<int64_t> free_at(static_cast<size_t>(at_once), 0);
+    auto later = [](int64_t a, int64_t b) { return a > b; };
+    for (const Tile &t : list) {
+        if (cutting && free_at.front() + t.k1 > share + share / 16 && t.k1 >= 2 * kLeast) {
+            cut.push_back(t);
+            cut_stages += t.k1;
+        } else {
+            std::pop_heap(free_at.begin(), free_at.end(), later);
+            free_at.back() += t.k1;
+            std::push_heap(free_at.begin(), free_at.end(), later);
+            whole.push_back(t);
+        }
+    }
+    const int64_t part = std::max<int64_t>(kLeast, (cut_stages + at_once - 1) / at_once);
+    for (const Tile &t : cut) {
+        const int32_t n = static_cast<int32_t>((t.k1 + part / 2) / part);
+        if (n < 2) {
+            pieces.push_back(t);
+            continue;
+        }
+        w.cuts.push_back(Cut{t.mat, t.i, t.j, w.slots, n, {0, 0, 0}});
+        for (int32_t p = 0; p < n; ++p) {
+            Tile q = t;
+            q.k0 = static_cast<int32_t>(static_cast<int64_t>(t.k1 / 2) * p / n) * 2;           // even numbers of stages
+            q.k1 = static_cast<int32_t>(static_cast<int64_t>(t.k1 / 2) * (p + 1) / n) * 2;
+            q.slot = w.slots++;
+            pieces.push_back(q);
+        }
+    }
+    w.tiles = by_xcd(whole);
+    const std::vector<Tile> rest = by_xcd(pieces);
+    w.tiles.insert(w.tiles.end(), rest.begin(), rest.end());
+}
+
+// The best of the sides, with and without cutting.
+void plan_product(const std::vector<Mat> &mats, int stage, bool split, Work &best)
+{
+    double least = 0.0;
+    for (int side : {64, 128, 256}) {
+        const std::vector<Tile> list = list_tiles(mats, side, stage, split ? kPanel<true> : kPanel<false>);
+        for (bool cutting : {false, true}) {
+            Work w;
+            deal_out(list, side, cutting, w);
+            if (cutting && w.cuts.empty()) continue;
+            double t = launch_time(w.tiles, side, split);
+            // the joining launch: itself, the parts' bytes, what it writes (the transposes two bytes at a time)
+            const double area = static_cast<double>(side) * side;
+            if (cutting) t += 5.5 + w.slots * area * 4.0 / 6e6 + static_cast<double>(w.cuts.size()) * area * 2.5e-6;
+            if (best.tiles.empty() || t < least) {
+                least = t;
+                best = std::move(w);
+            }
+        }
+    }
 }
 
 void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
@@ -661,23 +871,30 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
         for (int32_t p = 0; p < M.parts; ++p) t.parts.push_back(int2{k, p});
         t.mats.push_back(M);
     }
-    t.square_side = tile_side(t.mats, true);
-    t.wide_side = tile_side(t.mats, false);
-    t.square = make_tiles(t.mats, t.square_side, true);
-    t.wide = make_tiles(t.mats, t.wide_side, false);
-    t.operands = make_tiles(t.mats, 64, false);
+    plan_product(t.mats, kGram, split, t.gram);
+    plan_product(t.mats, kPoly, split, t.poly);
+    plan_product(t.mats, kApply, split, t.wide);
+    t.operands = by_xcd(list_tiles(t.mats, 64, kApply, kPanel<true>));
+}
+
+template <int SIDE, bool SPLIT, int STAGE, int OUT>
+void product_of(const ds_ortho *o, const ds_ortho::Launch &l, const Step &s, const Out &out, hipStream_t st)
+{
+    constexpr int WM = SIDE == 64 ? 32 : SIDE == 128 ? 64 : 128, WN = SIDE == 64 ? 32 : 64, THREADS = (SIDE / WM) * (SIDE / WN) * 64;
+    k_ortho_product<SIDE, SIDE, WM, WN, 4, SPLIT, STAGE, OUT><<<l.n_tiles, THREADS, 0, st>>>(o->mats, l.tiles, o->ws, o->sums, s, out);
+    if (l.n_cuts)
+        k_ortho_join<SIDE, SPLIT, STAGE, OUT><<<l.n_cuts * (SIDE * SIDE / 8 / kThreads), kThreads, 0, st>>>(o->mats, l.cuts, o->ws, o->sums, s,
+                                                                                                         out);
 }
 
 template <bool SPLIT, int STAGE, int OUT>
 void product(const ds_ortho *o, const Step &s, const Out &out, hipStream_t st)
 {
-    constexpr bool WIDE = STAGE >= kApply;
-    const Tile *tiles = WIDE ? o->wide : o->square;
-    const unsigned n = static_cast<unsigned>(WIDE ? o->n_wide : o->n_square);
-    switch (WIDE ? o->wide_side : o->square_side) {
-    case 256: k_ortho_product<256, 256, 128, 64, 4, SPLIT, STAGE, OUT><<<n, 512, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
-    case 128: k_ortho_product<128, 128, 64, 64, 4, SPLIT, STAGE, OUT><<<n, 256, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
-    default: k_ortho_product<64, 64, 32, 32, 4, SPLIT, STAGE, OUT><<<n, 256, 0, st>>>(o->mats, tiles, o->ws, s, out); break;
+    const ds_ortho::Launch &l = STAGE == kGram ? o->gram : STAGE == kPoly ? o->poly : o->wide;
+    switch (l.side) {
+    case 256: return product_of<256, SPLIT, STAGE, OUT>(o, l, s, out, st);
+    case 128: return product_of<128, SPLIT, STAGE, OUT>(o, l, s, out, st);
+    default: return product_of<64, SPLIT, STAGE, OUT>(o, l, s, out, st);
     }
 }
 
@@ -760,12 +977,8 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
         for (int32_t k = 0; k < 3 * cfg->steps; ++k) o->coef.push_back(cfg->coef ? cfg->coef[k] : standard[k % 3]);
         Tables t;
         make_tables(*cfg, o->split, t);
-        o->n_square = static_cast<int64_t>(t.square.size());
-        o->n_wide = static_cast<int64_t>(t.wide.size());
         o->n_operands = static_cast<int64_t>(t.operands.size());
         o->n_parts = static_cast<int64_t>(t.parts.size());
-        o->square_side = t.square_side;
-        o->wide_side = t.wide_side;
         int64_t bytes = 0;
         auto take = [&](int64_t b) {
             const int64_t at = bytes;
@@ -773,9 +986,17 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
             return at;
         };
         auto size_of = [](const auto &v) { return static_cast<int64_t>(v.size() * sizeof(v[0])); };
-        const int64_t at_mats = take(size_of(t.mats)), at_square = take(size_of(t.square)), at_wide = take(size_of(t.wide)),
-                      at_operands = take(size_of(t.operands)), at_parts = take(size_of(t.parts)), at_inside = take(size_of(plane));
-        const int64_t at_partial = take(t.n_partial * 8), at_u = take(cfg->d * 4), at_ws = take(t.ws_bytes);
+        Work *const works[3] = {&t.gram, &t.poly, &t.wide};
+        ds_ortho::Launch *const launches[3] = {&o->gram, &o->poly, &o->wide};
+        int64_t at_tiles[3], at_cuts[3], sum_bytes = 0;
+        for (int k = 0; k < 3; ++k) {
+            at_tiles[k] = take(size_of(works[k]->tiles));
+            at_cuts[k] = take(size_of(works[k]->cuts));
+            sum_bytes = std::max<int64_t>(sum_bytes, static_cast<int64_t>(works[k]->slots) * works[k]->side * works[k]->side * 4);
+        }
+        const int64_t at_mats = take(size_of(t.mats)), at_operands = take(size_of(t.operands)), at_parts = take(size_of(t.parts)),
+                      at_inside = take(size_of(plane));
+        const int64_t at_partial = take(t.n_partial * 8), at_u = take(cfg->d * 4), at_sums = take(sum_bytes), at_ws = take(t.ws_bytes);
         ds_status_t rc = hipGetDevice(&o->device) == hipSuccess ? DS_OK : DS_ERR_DEVICE;
         if (rc == DS_OK && hipMalloc(&o->mem, static_cast<size_t>(bytes)) != hipSuccess) {
             o->mem = nullptr;
@@ -784,11 +1005,15 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
         }
         char *base = static_cast<char *>(o->mem);
         auto put = [&](int64_t at, const auto &v) {
-            if (rc == DS_OK && hipMemcpy(base + at, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice) != hipSuccess) rc = DS_ERR_DEVICE;
+            if (rc == DS_OK && !v.empty() && hipMemcpy(base + at, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice) != hipSuccess) rc = DS_ERR_DEVICE;
         };
         put(at_mats, t.mats);
-        put(at_square, t.square);
-        put(at_wide, t.wide);
+        for (int k = 0; k < 3; ++k) {
+            put(at_tiles[k], works[k]->tiles);
+            put(at_cuts[k], works[k]->cuts);
+            *launches[k] = {reinterpret_cast<const Tile *>(base + at_tiles[k]), reinterpret_cast<const Cut *>(base + at_cuts[k]),
+                            static_cast<unsigned>(works[k]->tiles.size()), static_cast<unsigned>(works[k]->cuts.size()), works[k]->side};
+        }
         put(at_operands, t.operands);
         put(at_parts, t.parts);
         put(at_inside, plane);
@@ -798,13 +1023,12 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
             return rc;
         }
         o->mats = reinterpret_cast<const Mat *>(base + at_mats);
-        o->square = reinterpret_cast<const Tile *>(base + at_square);
-        o->wide = reinterpret_cast<const Tile *>(base + at_wide);
         o->operands = reinterpret_cast<const Tile *>(base + at_operands);
         o->parts = reinterpret_cast<const int2 *>(base + at_parts);
         o->inside = reinterpret_cast<uint64_t *>(base + at_inside);
         o->partial = reinterpret_cast<double *>(base + at_partial);
         o->u = reinterpret_cast<float *>(base + at_u);
+        o->sums = reinterpret_cast<float *>(base + at_sums);
         o->ws = base + at_ws;
     } catch (...) {
         ds_ortho_destroy(o);
