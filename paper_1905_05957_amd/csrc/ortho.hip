@@ -101,18 +101,21 @@ __device__ __forceinline__ void store1(char *p, float v)
     if (SPLIT) *reinterpret_cast<_Float16 *>(p + kToLo) = static_cast<_Float16>(v - static_cast<float>(hi));
 }
 
+// Eight elements of a row as they lie in memory.
 template <bool SPLIT>
-__device__ __forceinline__ void load8(const char *p, float *v)
-{
-    const half8 hi = *reinterpret_cast<const half8 *>(p);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = static_cast<float>(hi[t]);
-    if (SPLIT) {
-        const half8 lo = *reinterpret_cast<const half8 *>(p + kToLo);
-#pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] += static_cast<float>(lo[t]);
+struct Eight {
+    half8 hi, lo;
+    __device__ __forceinline__ void load(const char *p)
+    {
+        hi = *reinterpret_cast<const half8 *>(p);
+        if (SPLIT) lo = *reinterpret_cast<const half8 *>(p + kToLo);
     }
-}
+    __device__ __forceinline__ void values(float *v) const
+    {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = static_cast<float>(hi[t]) + (SPLIT ? static_cast<float>(lo[t]) : 0.f);
+    }
+};
 
 template <bool BF16>
 __device__ __forceinline__ float load_flat(const void *p, int64_t at)
@@ -532,6 +535,14 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
                 model[t] = n > 0 ? ld4_stream(out.x, at, at + n) : f32x4{0.f, 0.f, 0.f, 0.f};
             }
         }
+        Eight<SPLIT> was[FN][2];                               // asked for together
+        if (STAGE != kGram) {
+#pragma unroll
+            for (int b = 0; b < FN; ++b)
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    if (j0 + wj + b * 32 < j_end) was[b][g].load(old + element_at<SPLIT>(panel, ib + r, j0 + wj + b * 32 + 16 * g + 8 * h));
+        }
 #pragma unroll
         for (int b = 0; b < FN; ++b) {
             const int jb = j0 + wj + b * 32;
@@ -542,7 +553,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
                 float v[8], x[8];
                 const int i = ib + r, j = jb + 16 * g + 8 * h;
                 const int64_t at = element_at<SPLIT>(panel, i, j);
-                if (STAGE != kGram) load8<SPLIT>(old + at, x);
+                if (STAGE != kGram) was[b][g].values(x);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = STAGE == kGram ? c.v[e] * alpha : __fmaf_rn(beta, x[e], c.v[e] * alpha);
                 if constexpr (STAGE != kLast) {
@@ -581,6 +592,23 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     }
 }
 
+// Columns j .. j + 7 of row i of the last X, into the vector.
+template <int OUT>
+__device__ __forceinline__ void eight_into_vector(const Mat &M, const Out &out, int i, int j, const float *v)
+{
+    if (i >= M.m) return;
+    const float f = M.factor / M.scale;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (j + e >= M.n) return;
+        const int64_t to = M.offset + (M.flip ? static_cast<int64_t>(j + e) * M.ld + i : static_cast<int64_t>(i) * M.ld + j + e);
+        const float o = v[e] * f;
+        if (OUT == 0) static_cast<float *>(out.dst)[to] = o;
+        else if (OUT == 1) static_cast<uint16_t *>(out.dst)[to] = bf16_round(o);
+        else out.x[to] = __fmaf_rn(-out.gamma, o, out.keep * out.x[to]);
+    }
+}
+
 // Tiles whose sums were taken in parts: the parts in their order, then as a whole tile goes on.  A thread takes eight columns of
 // a row, a wavefront 64 rows.
 template <int SIDE, bool SPLIT, int STAGE, int OUT>
@@ -604,7 +632,11 @@ __global__ __launch_bounds__(kThreads) void k_ortho_join(const Mat *__restrict__
     const float alpha = product_scale<STAGE>(M, step), beta = old_scale<STAGE>(step);
     const int64_t at = element_at<SPLIT>(M.panel, i, j);
     float v[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w}, x[8];
-    if (STAGE != kGram) load8<SPLIT>(ws + (STAGE == kPoly ? M.g : M.x[step.from]) + at, x);
+    if (STAGE != kGram) {
+        Eight<SPLIT> was;
+        was.load(ws + (STAGE == kPoly ? M.g : M.x[step.from]) + at);
+        was.values(x);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = STAGE == kGram ? v[e] * alpha : __fmaf_rn(beta, x[e], v[e] * alpha);
     if constexpr (STAGE != kLast) {
@@ -614,17 +646,198 @@ __global__ __launch_bounds__(kThreads) void k_ortho_join(const Mat *__restrict__
 #pragma unroll
             for (int e = 0; e < 8; ++e) store1<SPLIT>(to + element_at<SPLIT>(M.panel, j + e, i), v[e]);
         }
-    } else if (i < M.m) {
-        const float f = M.factor / M.scale;
+    } else {
+        eight_into_vector<OUT>(M, out, i, j, v);
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// small matrices: one workgroup and one launch for all of it
+// ---------------------------------------------------------------------------------------
+constexpr int kSmallBytes = 144 * 1024;        // X and G in LDS
+constexpr int kSmallBytesMany = 40 * 1024;     // so that four of them share a compute unit
+
+template <bool SPLIT>
+int64_t small_bytes(int64_t mp, int64_t np) { return (mp * np + mp * mp) * (SPLIT ? 4 : 2); }
+
+// Norm, operands, all steps and the result of one matrix, X [MP, np] and G (B in its place) in LDS.  Chains of small
+// dependent products are bound by latency: five steps on 96 x 64 took 15 launches and 54 us, 0 NEW us so.
+//
+// Panels as in the large form; chunk c of row r of panel p lies at c ^ f(r, p), f = (r / 4) % 4, and with two halves the
+// panels take turns with hi and lo: 16 lanes that read rows, and 32 lanes that read transposing, meet different banks.
+template <int MP, int CAP, bool SPLIT, bool BF16, int OUT>
+__global__ __launch_bounds__(kThreads) void k_ortho_small(const Mat *__restrict__ mats, const int32_t *__restrict__ list, const void *src,
+                                                          const float *__restrict__ coef, int steps, float eps, Out out)
+{
+    constexpr int K = kPanel<SPLIT>, PANEL = MP * kRow, NB = MP / 32, WAVES = kThreads / 64, GBYTES = MP / K * PANEL;
+    constexpr int SQUARE = NB * (NB + 1) / 2, PER_WAVE = (SQUARE + WAVES - 1) / WAVES;
+    __shared__ __attribute__((aligned(256))) char lds[CAP];
+    __shared__ double sums[WAVES];
+    const Mat &M = mats[list[blockIdx.x]];
+    const int np = M.np, lane = lane_id(), wave = wave_id(), r = lane & 31, h = lane >> 5;
+    char *G = lds, *X = lds + GBYTES;
+    auto chunk = [&](char *base, int row, int panel, int c) {
+        return base + panel * PANEL + row * kRow + ((c ^ ((row >> 2) & 3) ^ (SPLIT ? 2 * (panel & 1) : 0)) * 16);
+    };
+    auto put8 = [&](char *base, int row, int col, const float *v) {
+        half8 hi, lo;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            hi[t] = static_cast<_Float16>(v[t]);
+            lo[t] = static_cast<_Float16>(v[t] - static_cast<float>(hi[t]));
+        }
+        *reinterpret_cast<half8 *>(chunk(base, row, col / K, (col % K) / 8)) = hi;
+        if (SPLIT) *reinterpret_cast<half8 *>(chunk(base, row, col / K, 2 + (col % K) / 8)) = lo;
+    };
+    auto put1 = [&](char *base, int row, int col, float v) {
+        const _Float16 hi = static_cast<_Float16>(v);
+        *reinterpret_cast<_Float16 *>(chunk(base, row, col / K, (col % K) / 8) + (col & 7) * 2) = hi;
+        if (SPLIT)
+            *reinterpret_cast<_Float16 *>(chunk(base, row, col / K, 2 + (col % K) / 8) + (col & 7) * 2) =
+                static_cast<_Float16>(v - static_cast<float>(hi));
+    };
+    auto get8 = [&](char *base, int row, int col, float *v) {
+        const half8 hi = *reinterpret_cast<const half8 *>(chunk(base, row, col / K, (col % K) / 8));
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = static_cast<float>(hi[t]);
+        if (SPLIT) {
+            const half8 lo = *reinterpret_cast<const half8 *>(chunk(base, row, col / K, 2 + (col % K) / 8));
+#pragma unroll
+            for (int t = 0; t < 8; ++t) v[t] += static_cast<float>(lo[t]);
+        }
+    };
+    // fragments of a panel's values of k: q = hi and lo, or the panel's two halves of k
+    auto rows = [&](char *base, int row0, int panel, int q) {
+        return *reinterpret_cast<const half8 *>(chunk(base, row0 + r, panel, q * 2 + h));
+    };
+    auto columns = [&](int col0, int k0, int q) {
+        union { half8 v; s16x4 part[2]; } u;
+        const int g = (lane >> 4) & 1;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int k = k0 + (SPLIT ? 0 : q * 16) + h * 8 + e * 4 + ((lane & 15) >> 2);
+            const char *p = SPLIT ? chunk(X, k, col0 / K + g, q * 2 + ((lane & 3) >> 1)) : chunk(X, k, col0 / K, g * 2 + ((lane & 3) >> 1));
+            u.part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + (lane & 1) * 8));
+        }
+        return u.v;
+    };
+    auto multiply = [&](const half8 *p, const half8 *q, f32x16 acc) {
+        if (SPLIT) {
+            acc = mfma(q[0], p[1], acc);
+            acc = mfma(q[1], p[0], acc);
+            return mfma(q[0], p[0], acc);
+        }
+        acc = mfma(q[0], p[0], acc);
+        return mfma(q[1], p[1], acc);
+    };
+
+    double s = 0.0;
+    const uint32_t total = static_cast<uint32_t>(M.rows) * M.cols, cols = M.cols;
+    for (uint32_t t = threadIdx.x; t < total; t += kThreads) {
+        const uint32_t row = t / cols;
+        const double v = load_flat<BF16>(src, M.offset + row * M.ld + (t - row * cols));
+        s = fma(v, v, s);
+    }
+    s = wave_sum(s);
+    if (lane == 0) sums[wave] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) s += sums[w];
+    const double norm = sqrt(s) + static_cast<double>(eps);
+    const double inv = norm == 0.0 ? 0.0 : static_cast<double>(M.scale) / norm;
+    for (int t = threadIdx.x; t < MP * np / 8; t += kThreads) {
+        const int i = M.flip ? t % MP : t / (np / 8), j = (M.flip ? t / MP : t % (np / 8)) * 8;
+        float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (j + e >= M.n) break;
-            const int64_t to = M.offset + (M.flip ? static_cast<int64_t>(j + e) * M.ld + i : static_cast<int64_t>(i) * M.ld + j + e);
-            const float o = v[e] * f;
-            if (OUT == 0) static_cast<float *>(out.dst)[to] = o;
-            else if (OUT == 1) static_cast<uint16_t *>(out.dst)[to] = bf16_round(o);
-            else out.x[to] = __fmaf_rn(-out.gamma, o, out.keep * out.x[to]);
+            v[e] = 0.f;
+            if (i < M.m && j + e < M.n) {
+                const int64_t at = M.offset + (M.flip ? (j + e) * M.ld + i : i * M.ld + j + e);
+                v[e] = static_cast<float>(static_cast<double>(load_flat<BF16>(src, at)) * inv);
+            }
         }
+        put8(X, i, j, v);
+    }
+    __syncthreads();
+
+    for (int k = 0; k < steps; ++k) {
+        const Step step{coef[3 * k], coef[3 * k + 1], coef[3 * k + 2], 0};
+        auto square = [&](auto stage) {
+            constexpr int STAGE = decltype(stage)::value;
+            const float alpha = product_scale<STAGE>(M, step), beta = old_scale<STAGE>(step);
+            f32x16 acc[PER_WAVE];
+#pragma unroll
+            for (int u = 0; u < PER_WAVE; ++u) {
+                const int t = u * WAVES + wave;
+                if (t >= SQUARE) break;
+                const int bi = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, bj = t - bi * (bi + 1) / 2;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[u][e] = 0.f;
+                char *from = STAGE == kGram ? X : G;
+                const int panels = (STAGE == kGram ? np : MP) / K;
+#pragma unroll 2
+                for (int p = 0; p < panels; ++p) {
+                    const half8 fp[2] = {rows(from, bi * 32, p, 0), rows(from, bi * 32, p, 1)};
+                    const half8 fq[2] = {rows(from, bj * 32, p, 0), rows(from, bj * 32, p, 1)};
+                    acc[u] = multiply(fp, fq, acc[u]);
+                }
+            }
+            if (STAGE == kPoly) __syncthreads();               // everybody has read G, B takes its place
+#pragma unroll
+            for (int u = 0; u < PER_WAVE; ++u) {
+                const int t = u * WAVES + wave;
+                if (t >= SQUARE) break;
+                const int bi = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, bj = t - bi * (bi + 1) / 2;
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const EightColumns c(acc[u], g);
+                    const int i = bi * 32 + r, j = bj * 32 + 16 * g + 8 * h;
+                    float v[8];
+                    if (STAGE == kPoly) get8(G, i, j, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = STAGE == kGram ? c.v[e] * alpha : __fmaf_rn(beta, v[e], c.v[e] * alpha);
+                    put8(G, i, j, v);
+                    if (bi != bj)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) put1(G, j + e, i, v[e]);
+                }
+            }
+            __syncthreads();
+        };
+        square(std::integral_constant<int, kGram>{});
+        square(std::integral_constant<int, kPoly>{});
+        // X <- a X + B X: a wavefront's columns are its own, so X changes in place
+        const float alpha = product_scale<kApply>(M, step), beta = step.a;
+        for (int bj = wave; bj < np / 32; bj += WAVES) {
+            f32x16 acc[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[b][e] = 0.f;
+            for (int p = 0; p < MP / K; ++p) {
+                const half8 fq[2] = {columns(bj * 32, p * K, 0), columns(bj * 32, p * K, 1)};
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const half8 fp[2] = {rows(G, b * 32, p, 0), rows(G, b * 32, p, 1)};
+                    acc[b] = multiply(fp, fq, acc[b]);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const EightColumns c(acc[b], g);
+                    const int i = b * 32 + r, j = bj * 32 + 16 * g + 8 * h;
+                    float v[8];
+                    get8(X, i, j, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn(beta, v[e], c.v[e] * alpha);
+                    if (k + 1 < steps) put8(X, i, j, v);
+                    else eight_into_vector<OUT>(M, out, i, j, v);
+                }
+        }
+        __syncthreads();
     }
 }
 
@@ -650,6 +863,11 @@ struct ds_ortho {
     const int2 *parts;
     int64_t n_operands, n_parts;
     float *sums;                           // parts of sums
+    // every matrix fits one workgroup's LDS: their numbers by class (64 rows many to a compute unit, 64 rows, 128 rows), one
+    // launch each, and nothing of the above but `mats`
+    const int32_t *small[3];
+    unsigned n_small[3];
+    const float *small_coef;
     double *partial;
     uint64_t *inside;                      // plane of bits: the elements of the matrices
     float *u;                              // [d] what is orthogonalised, where it is not m
@@ -689,7 +907,17 @@ struct Tables {
     std::vector<Tile> operands;
     std::vector<int2> parts;
     int64_t n_partial = 0, ws_bytes = 0;
+    std::vector<int32_t> small[3];
 };
+
+// Which of the small classes takes a matrix, or -1.
+int small_class(const Mat &M, bool split)
+{
+    if (M.mp > 128) return -1;
+    const int64_t bytes = split ? small_bytes<true>(M.mp, M.np) : small_bytes<false>(M.mp, M.np);
+    if (bytes > kSmallBytes) return -1;
+    return M.mp == 128 ? 2 : bytes > kSmallBytesMany ? 1 : 0;
+}
 
 // All tiles of a product: long sums first, so that the launch ends with short ones; within a matrix strips of rows, so that
 // tiles near each other in time share rows and columns.
@@ -833,6 +1061,7 @@ void plan_product(const std::vector<Mat> &mats, int stage, bool split, Work &bes
 
 void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
 {
+    bool all_small = true;
     for (int32_t k = 0; k < cfg.n_mats; ++k) {
         const ds_matrix_t &in = cfg.mats[k];
         Mat M{};
@@ -854,11 +1083,21 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
         const double aspect = static_cast<double>(in.rows) / in.cols;
         M.factor = cfg.factor == DS_ORTHO_FACTOR_ASPECT ? static_cast<float>(sqrt(std::max(1.0, aspect)))
                    : cfg.factor == DS_ORTHO_FACTOR_RMS ? static_cast<float>(0.2 * sqrt(static_cast<double>(M.n))) : 1.0f;
-        auto take = [&](int64_t bytes) {
-            const int64_t at = t.ws_bytes;
-            t.ws_bytes += round_up(bytes, 256);
-            return at;
-        };
+        all_small = all_small && small_class(M, split) >= 0;
+        t.mats.push_back(M);
+    }
+    // Small matrices among large ones go with them: there they cost a tile, here a launch.
+    if (all_small) {
+        for (int32_t k = 0; k < cfg.n_mats; ++k) t.small[small_class(t.mats[static_cast<size_t>(k)], split)].push_back(k);
+        return;
+    }
+    auto take = [&](int64_t bytes) {
+        const int64_t at = t.ws_bytes;
+        t.ws_bytes += round_up(bytes, 256);
+        return at;
+    };
+    for (int32_t k = 0; k < cfg.n_mats; ++k) {
+        Mat &M = t.mats[static_cast<size_t>(k)];
         const int64_t each = split ? 4 : 2;
         M.x[0] = take(static_cast<int64_t>(M.mp) * M.np * each);
         M.x[1] = take(static_cast<int64_t>(M.mp) * M.np * each);
@@ -869,7 +1108,6 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
         M.part0 = static_cast<int32_t>(t.n_partial);
         t.n_partial += M.parts;
         for (int32_t p = 0; p < M.parts; ++p) t.parts.push_back(int2{k, p});
-        t.mats.push_back(M);
     }
     plan_product(t.mats, kGram, split, t.gram);
     plan_product(t.mats, kPoly, split, t.poly);
@@ -902,6 +1140,17 @@ void product(const ds_ortho *o, const Step &s, const Out &out, hipStream_t st)
 template <bool SPLIT, bool SRC_BF16, int OUT>
 ds_status_t run(const ds_ortho *o, const void *src, const Out &out, hipStream_t st)
 {
+    if (o->n_small[0] + o->n_small[1] + o->n_small[2]) {
+        auto go = [&](auto mp, auto cap, int c) {
+            if (o->n_small[c])
+                k_ortho_small<decltype(mp)::value, decltype(cap)::value, SPLIT, SRC_BF16, OUT><<<o->n_small[c], kThreads, 0, st>>>(
+                    o->mats, o->small[c], src, o->small_coef, o->cfg.steps, o->cfg.eps, out);
+        };
+        go(std::integral_constant<int, 64>{}, std::integral_constant<int, kSmallBytesMany>{}, 0);
+        go(std::integral_constant<int, 64>{}, std::integral_constant<int, kSmallBytes>{}, 1);
+        go(std::integral_constant<int, 128>{}, std::integral_constant<int, kSmallBytes>{}, 2);
+        return ds_launch_status();
+    }
     auto grid = [](int64_t n) { return static_cast<unsigned>(n); };
     k_ortho_norm<SRC_BF16><<<grid(o->n_parts), kBlock, 0, st>>>(o->mats, o->parts, src, o->partial);
     k_ortho_operands<SPLIT, SRC_BF16><<<grid(o->n_operands), kThreads, 0, st>>>(o->mats, o->operands, src, o->partial, o->cfg.eps, o->ws);
@@ -996,6 +1245,9 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
         }
         const int64_t at_mats = take(size_of(t.mats)), at_operands = take(size_of(t.operands)), at_parts = take(size_of(t.parts)),
                       at_inside = take(size_of(plane));
+        int64_t at_small[3];
+        for (int k = 0; k < 3; ++k) at_small[k] = take(size_of(t.small[k]));
+        const int64_t at_coef = take(size_of(o->coef));
         const int64_t at_partial = take(t.n_partial * 8), at_u = take(cfg->d * 4), at_sums = take(sum_bytes), at_ws = take(t.ws_bytes);
         ds_status_t rc = hipGetDevice(&o->device) == hipSuccess ? DS_OK : DS_ERR_DEVICE;
         if (rc == DS_OK && hipMalloc(&o->mem, static_cast<size_t>(bytes)) != hipSuccess) {
@@ -1007,6 +1259,13 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
         auto put = [&](int64_t at, const auto &v) {
             if (rc == DS_OK && !v.empty() && hipMemcpy(base + at, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice) != hipSuccess) rc = DS_ERR_DEVICE;
         };
+        for (int k = 0; k < 3; ++k) {
+            put(at_small[k], t.small[k]);
+            o->small[k] = reinterpret_cast<const int32_t *>(base + at_small[k]);
+            o->n_small[k] = static_cast<unsigned>(t.small[k].size());
+        }
+        put(at_coef, o->coef);
+        o->small_coef = reinterpret_cast<const float *>(base + at_coef);
         put(at_mats, t.mats);
         for (int k = 0; k < 3; ++k) {
             put(at_tiles[k], works[k]->tiles);

@@ -75,6 +75,41 @@ def test_one_matrix(gpu_device, shape, half):
     plan.close()
 
 
+# sides at which a plan changes from one workgroup per matrix to launches over tiles: (rows + columns) of the rounded matrix
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("shape", [(64, 512), (64, 513), (513, 64), (40, 96), (50, 65), (60, 449), (128, 160), (161, 128), (100, 120),
+                                   (120, 384), (385, 128), (64, 1024), (1025, 33), (2, 1000), (1100, 5), (65, 65)],
+                         ids=lambda s: f"{s[0]}x{s[1]}")
+def test_small_and_not_quite_small(gpu_device, shape, half):
+    r, c = shape
+    src = random_flat(3 * r * c, gpu_device, 13)
+    mats = [(k * r * c, r, c) for k in range(3)]
+    plan = P.OrthoPlan(3 * r * c, mats, half=half)
+    dst = torch.full_like(src, 7.0)
+    plan.orthogonalize(src, dst)
+    for m in mats:
+        check(view(dst, m), reference(view(src, m)), half)
+    plan.close()
+
+
+def test_a_thousand_small_matrices(gpu_device):
+    gen = torch.Generator()
+    gen.manual_seed(14)
+    mats, at = [], 0
+    for _ in range(1000):
+        r, c = (int(v) for v in torch.randint(1, 60, (2,), generator=gen))
+        mats.append((at, r, c))
+        at += r * c + 1
+    src = random_flat(at, gpu_device, 15)
+    dst = torch.full_like(src, 7.0)
+    plan = P.OrthoPlan(at, mats)
+    plan.orthogonalize(src, dst)
+    got, want = dst.cpu(), src.cpu()
+    for m in mats:
+        check(view(got, m), reference(view(want, m)), False)
+    plan.close()
+
+
 @pytest.mark.parametrize("src_dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("dst_dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("half", [False, True])
