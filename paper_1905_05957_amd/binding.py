@@ -132,7 +132,7 @@ def _load_fastcall():
         L = load_library()
         _fastcall = Calls, [C.cast(f, C.c_void_p).value for f in (
             L.ds_worker_compress, L.ds_server_aggregate_compress, L.ds_apply_update, L.ds_decompress,
-            L.ds_server_aggregate_compress_update)]
+            L.ds_server_aggregate_compress_update, L.ds_apply_update_ortho, L.ds_apply_update_adamw)]
     return _fastcall
 
 
@@ -288,8 +288,9 @@ class Context:
         self.no_error_feedback = bool(int(flags) & FLAG_NO_ERROR_FEEDBACK)
         self.server_identity = bool(int(flags) & FLAG_SERVER_IDENTITY)
         make_calls, address = _load_fastcall()
+        self.device = torch.device("cuda", torch._C._cuda_getDevice())
         self._calls = make_calls(self._h.value, self.n, self.d, self.k, self.comp, self.grad_dtype == BF16,
-                                 self.no_error_feedback, self.server_identity, Payload, torch._C._cuda_getDevice,
+                                 self.no_error_feedback, self.server_identity, self.device.index, Payload, torch._C._cuda_getDevice,
                                  torch._C._cuda_getCurrentRawStream, *address)
 
     def close(self):
@@ -384,42 +385,47 @@ class Context:
                                               None if m is None else m.data_ptr(), gamma, beta,
                                               _stream_ptr(stream)), "ds_apply_update")
 
-    def _same_vector(self, plan: "OrthoPlan") -> "OrthoPlan":
-        if not isinstance(plan, OrthoPlan) or plan._h.value is None:
+    def _plan_address(self, plan: "OrthoPlan") -> int:
+        if not isinstance(plan, OrthoPlan) or not plan._h.value:
             raise ValueError("plan: an open OrthoPlan is required")
-        if plan.d != self.d:
-            raise ValueError(f"plan: made for a vector of {plan.d} elements, the context for {self.d}")
-        return plan
+        if plan.d != self.d or plan.device != self.device:
+            raise ValueError(f"plan: made for {plan.d} elements on {plan.device}, the context for {self.d} on {self.device}")
+        return plan._h.value
 
     def apply_update_ortho(self, plan: "OrthoPlan", srv: Payload, x: torch.Tensor, m: Optional[torch.Tensor], gamma: float,
                            beta: float = 0.0, decay: float = 0.0, stream=None):
         """The model update through the plan's matrices: momentum, orthogonalisation, weights.  Elements outside them stay."""
-        self._same_vector(plan)
+        address = self._plan_address(plan)
+        rc = self._calls.ortho(address, srv, x, m, gamma, beta, decay, stream)
+        if rc >= 0:
+            return _check(rc, "ds_apply_update_ortho")
         _need(x, "x", torch.float32, (self.d,))
         if m is not None:
             _need(m, "m", torch.float32, (self.d,))
         s = srv.check(self, 1, "srv", server=True)
-        _one_device(plan.device, x=x, m=m, **s.tensors())
+        _one_device(self.device, x=x, m=m, **s.tensors())
         s = s.c_struct()
-        _check(load_library().ds_apply_update_ortho(self._h, plan._h, C.byref(s), x.data_ptr(), None if m is None else m.data_ptr(),
-                                                    gamma, beta, decay, _stream_ptr(stream, plan.device)), "ds_apply_update_ortho")
+        _check(load_library().ds_apply_update_ortho(self._h, address, C.byref(s), x.data_ptr(), None if m is None else m.data_ptr(),
+                                                    gamma, beta, decay, _stream_ptr(stream, self.device)), "ds_apply_update_ortho")
 
     def apply_update_adamw(self, srv: Payload, step: int, x: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gamma: float,
                            beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, decay: float = 0.0,
                            skip: Optional["OrthoPlan"] = None, stream=None):
         """The model update by AdamW, on every element or on those outside the matrices of `skip`; `step` counts from 0."""
-        if skip is not None:
-            self._same_vector(skip)
+        address = 0 if skip is None else self._plan_address(skip)
+        rc = self._calls.adamw(address, srv, step, x, m, v, gamma, beta1, beta2, eps, decay, stream)
+        if rc >= 0:
+            return _check(rc, "ds_apply_update_adamw")
         for t, what in ((x, "x"), (m, "m"), (v, "v")):
             _need(t, what, torch.float32, (self.d,))
-        if int(step) < 0:
+        if not 0 <= int(step) < 1 << 64:
             raise ValueError("step: counts from 0")
         s = srv.check(self, 1, "srv", server=True)
-        _one_device(x.device if skip is None else skip.device, x=x, m=m, v=v, **s.tensors())
+        _one_device(self.device, x=x, m=m, v=v, **s.tensors())
         s = s.c_struct()
-        _check(load_library().ds_apply_update_adamw(self._h, None if skip is None else skip._h, C.byref(s), int(step), x.data_ptr(),
-                                                    m.data_ptr(), v.data_ptr(), gamma, beta1, beta2, eps, decay,
-                                                    _stream_ptr(stream, x.device)), "ds_apply_update_adamw")
+        _check(load_library().ds_apply_update_adamw(self._h, address, C.byref(s), int(step), x.data_ptr(), m.data_ptr(), v.data_ptr(),
+                                                    gamma, beta1, beta2, eps, decay, _stream_ptr(stream, self.device)),
+               "ds_apply_update_adamw")
 
     def materialize_error(self, delta: Optional[torch.Tensor], delta_s: Optional[torch.Tensor],
                           stream=None):

@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kBlock) void k_clip_update(const uint8_t *msg, floa
 template <int NB, class Tail>
 __global__ __launch_bounds__(kBlock) void k_clip_each(const uint8_t *msg, int64_t d, Tail tail)
 {
-    const int64_t e = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    const int64_t e = tail.first() + threadIdx.x * 4;
     if (e >= d) return;
     const uint32_t f = tail.wants(e, d);
     if (f) tail.put(load_msg4<NB>(msg, e, d), e, d, f);
@@ -326,7 +326,7 @@ template <class Tail>
 ds_status_t ds_clip_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
 {
     with_bytes(c->cfg.levels, [&](auto nb) {
-        k_clip_each<decltype(nb)::value><<<blocks4(c->cfg.d), kBlock, 0, st>>>(srv->levels, c->cfg.d, tail);
+        k_clip_each<decltype(nb)::value><<<static_cast<unsigned>(tail.n), kBlock, 0, st>>>(srv->levels, c->cfg.d, tail);
     });
     return ds_launch_status();
 }

@@ -412,7 +412,9 @@ ds_status_t ds_apply_update_ortho(ds_ctx_t *c, ds_ortho_t *plan, const ds_payloa
     if (!guard.ok) return DS_ERR_DEVICE;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     float *u = !m || ds_ortho_nesterov(plan) ? ds_ortho_buffer(plan) : nullptr;
-    const ds_status_t done = each(c, srv, ds::TailMomentum{ds_ortho_inside(plan), m, u, beta}, st);
+    ds::TailTiles tiles;
+    tiles.tiles = ds_ortho_tiles(plan, true, &tiles.n);
+    const ds_status_t done = each(c, srv, ds::TailMomentum{tiles, ds_ortho_inside(plan), m, u, beta}, st);
     if (done != DS_OK) return done;
     return ds_ortho_update(plan, u ? u : m, x, gamma, decay, st);
 }
@@ -430,7 +432,10 @@ ds_status_t ds_apply_update_adamw(ds_ctx_t *c, const ds_ortho_t *skip, const ds_
     DeviceGuard guard(c->device);
     if (!guard.ok) return DS_ERR_DEVICE;
     const double t = static_cast<double>(step) + 1.0;
-    const ds::TailAdamW tail{skip ? ds_ortho_inside(skip) : nullptr, x, m, v, static_cast<float>(beta1),
+    ds::TailTiles tiles{nullptr, static_cast<int32_t>(c->n_tiles)};
+    if (skip) tiles.tiles = ds_ortho_tiles(skip, false, &tiles.n);
+    if (tiles.n == 0) return DS_OK;                                         // the matrices are all of it
+    const ds::TailAdamW tail{tiles, skip ? ds_ortho_inside(skip) : nullptr, x, m, v, static_cast<float>(beta1),
                              static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
                              static_cast<float>(gamma / (1.0 - pow(beta1, t))), static_cast<float>(1.0 / sqrt(1.0 - pow(beta2, t))),
                              static_cast<float>(eps), static_cast<float>(1.0 - gamma * decay)};

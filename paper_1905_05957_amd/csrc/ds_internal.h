@@ -208,6 +208,8 @@ template <class Tail> ds_status_t ds_rsparse_each(ds_ctx *c, const ds_payload_t 
 // ortho.hip: what the update calls need of a plan, and the matrices of `u` orthogonalised into the model
 // (x <- (1 - gamma * decay) x - gamma O(u)).
 const uint64_t *ds_ortho_inside(const ds_ortho *o);      // plane of bits: the elements of its matrices
+// 2048-element tiles of the vector with an element of a matrix (inside) or of none, on the device
+const int32_t *ds_ortho_tiles(const ds_ortho *o, bool inside, int32_t *n);
 int64_t ds_ortho_elements(const ds_ortho *o);
 int ds_ortho_device(const ds_ortho *o);
 bool ds_ortho_nesterov(const ds_ortho *o);

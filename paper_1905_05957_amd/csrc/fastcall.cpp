@@ -23,6 +23,9 @@ using UpdateFn = ds_status_t (*)(ds_ctx_t *, const ds_payload_t *, float *, floa
 using DecodeFn = ds_status_t (*)(ds_ctx_t *, const ds_payload_t *, int32_t, int32_t, float *, void *);
 using ServerUpdateFn = ds_status_t (*)(ds_ctx_t *, uint64_t, const ds_payload_t *, float *, const ds_payload_t *, float *, float *, float,
                                        float, void *);
+using OrthoFn = ds_status_t (*)(ds_ctx_t *, ds_ortho_t *, const ds_payload_t *, float *, float *, float, float, float, void *);
+using AdamWFn = ds_status_t (*)(ds_ctx_t *, const ds_ortho_t *, const ds_payload_t *, uint64_t, float *, float *, float *, double, double,
+                                double, double, double, void *);
 
 struct Calls {
     PyObject_HEAD
@@ -36,6 +39,9 @@ struct Calls {
     UpdateFn update;
     DecodeFn decode;
     ServerUpdateFn server_update;
+    OrthoFn ortho;
+    AdamWFn adamw;
+    int device;
 };
 
 constexpr int kIdentity = 0;
@@ -80,8 +86,8 @@ bool int_attr(PyObject *o, PyObject *name, int64_t *out)
     return ok;
 }
 
-// rows < 0: as many as the payload says.
-bool payload(const Calls *c, PyObject *o, int64_t rows, bool server, ds_payload_t *out, int64_t *rows_out = nullptr)
+// rows < 0: as many as the payload says.  device >= 0: the buffers have to be there.
+bool payload(const Calls *c, PyObject *o, int64_t rows, bool server, ds_payload_t *out, int64_t *rows_out = nullptr, int device = -1)
 {
     if (reinterpret_cast<PyObject *>(Py_TYPE(o)) != c->payload_type) return false;
     int64_t comp, has_rows, d, k;
@@ -98,7 +104,7 @@ bool payload(const Calls *c, PyObject *o, int64_t rows, bool server, ds_payload_
         bool ok = true;
         if (v != Py_None) {
             const at::Tensor *t = device_tensor(v);
-            ok = t && t->is_contiguous();
+            ok = t && t->is_contiguous() && (device < 0 || t->get_device() == device);
             if (ok) p[i] = t->data_ptr();
         }
         Py_DECREF(v);                                // the payload holds it
@@ -109,13 +115,18 @@ bool payload(const Calls *c, PyObject *o, int64_t rows, bool server, ds_payload_
     return true;
 }
 
-// The stream to launch on: the one given, or the current one of the current device.
-bool stream(const Calls *c, PyObject *o, void **out)
+// The stream to launch on: the one given, or the current one of the current device, which is to be `device` if that is >= 0.
+bool stream(const Calls *c, PyObject *o, void **out, int device = -1)
 {
     PyObject *v;
     if (o == Py_None) {
         PyObject *dev = PyObject_CallNoArgs(c->get_device);
         if (!dev) { PyErr_Clear(); return false; }
+        if (device >= 0 && !(PyLong_CheckExact(dev) && PyLong_AsLong(dev) == device)) {
+            Py_DECREF(dev);
+            PyErr_Clear();
+            return false;
+        }
         v = PyObject_CallOneArg(c->get_stream, dev);
         Py_DECREF(dev);
     } else {
@@ -141,6 +152,32 @@ bool number(PyObject *o, float *out)
     if (PyFloat_CheckExact(o)) *out = static_cast<float>(PyFloat_AS_DOUBLE(o));
     else if (PyLong_CheckExact(o)) *out = static_cast<float>(PyLong_AsDouble(o));
     else return false;
+    if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+    return true;
+}
+
+bool number(PyObject *o, double *out)
+{
+    if (PyFloat_CheckExact(o)) *out = PyFloat_AS_DOUBLE(o);
+    else if (PyLong_CheckExact(o)) *out = PyLong_AsDouble(o);
+    else return false;
+    if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+    return true;
+}
+
+// A vector of d floats on the context's device.
+bool own_vector(const Calls *c, PyObject *o, float **out)
+{
+    *out = static_cast<float *>(matrix(o, at::kFloat, 0, c->d, nullptr));
+    return *out != nullptr && THPVariable_Unpack(o).get_device() == c->device;
+}
+
+// A plan's address; the caller has seen that the plan is open and fits.
+template <class T>
+bool address(PyObject *o, T **out)
+{
+    if (!PyLong_CheckExact(o)) return false;
+    *out = static_cast<T *>(PyLong_AsVoidPtr(o));
     if (PyErr_Occurred()) { PyErr_Clear(); return false; }
     return true;
 }
@@ -249,6 +286,46 @@ PyObject *update(PyObject *self, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
+// plan, srv, x, m, gamma, beta, decay, stream
+PyObject *ortho(PyObject *self, PyObject *const *a, Py_ssize_t nargs)
+{
+    return call(self, nargs, 8, [a](const Calls *c, ds_status_t &rc) {
+        void *st;
+        ds_ortho_t *plan;
+        float *x, *m = nullptr, gamma, beta, decay;
+        ds_payload_t srv;
+        if (!address(a[0], &plan) || !own_vector(c, a[2], &x) || (a[3] != Py_None && !own_vector(c, a[3], &m))) return false;
+        if (!number(a[4], &gamma) || !number(a[5], &beta) || !number(a[6], &decay)) return false;
+        if (!payload(c, a[1], 1, true, &srv, nullptr, c->device) || !stream(c, a[7], &st, c->device)) return false;
+        Py_BEGIN_ALLOW_THREADS
+        rc = c->ortho(c->ctx, plan, &srv, x, m, gamma, beta, decay, st);
+        Py_END_ALLOW_THREADS
+        return true;
+    });
+}
+
+// plan or 0, srv, step, x, m, v, gamma, beta1, beta2, eps, decay, stream
+PyObject *adamw(PyObject *self, PyObject *const *a, Py_ssize_t nargs)
+{
+    return call(self, nargs, 12, [a](const Calls *c, ds_status_t &rc) {
+        void *st;
+        ds_ortho_t *plan;
+        float *x, *m, *v;
+        double gamma, beta1, beta2, eps, decay;
+        ds_payload_t srv;
+        if (!address(a[0], &plan) || !PyLong_CheckExact(a[2])) return false;
+        const unsigned long long t = PyLong_AsUnsignedLongLong(a[2]);
+        if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+        if (!own_vector(c, a[3], &x) || !own_vector(c, a[4], &m) || !own_vector(c, a[5], &v)) return false;
+        if (!number(a[6], &gamma) || !number(a[7], &beta1) || !number(a[8], &beta2) || !number(a[9], &eps) || !number(a[10], &decay)) return false;
+        if (!payload(c, a[1], 1, true, &srv, nullptr, c->device) || !stream(c, a[11], &st, c->device)) return false;
+        Py_BEGIN_ALLOW_THREADS
+        rc = c->adamw(c->ctx, plan, &srv, t, x, m, v, gamma, beta1, beta2, eps, decay, st);
+        Py_END_ALLOW_THREADS
+        return true;
+    });
+}
+
 // p, row, out, stream
 PyObject *decode(PyObject *self, PyObject *const *a, Py_ssize_t nargs)
 {
@@ -275,16 +352,16 @@ PyObject *close_calls(PyObject *self, PyObject *)
     Py_RETURN_NONE;
 }
 
-// Calls(context, n, d, k, comp, bf16, nofb, sid, payload_type, get_device, get_stream, addresses of the five functions)
+// Calls(context, n, d, k, comp, bf16, nofb, sid, device, payload_type, get_device, get_stream, addresses of the seven functions)
 int init_calls(PyObject *self, PyObject *args, PyObject *)
 {
     Calls *c = reinterpret_cast<Calls *>(self);
-    unsigned long long ctx, f[5];
+    unsigned long long ctx, f[7];
     long long n, d, k;
     int bf16, nofb, sid;
     PyObject *type, *dev, *str;
-    if (!PyArg_ParseTuple(args, "KLLLipppOOOKKKKK", &ctx, &n, &d, &k, &c->comp, &bf16, &nofb, &sid, &type, &dev, &str, &f[0], &f[1], &f[2],
-                          &f[3], &f[4]))
+    if (!PyArg_ParseTuple(args, "KLLLipppiOOOKKKKKKK", &ctx, &n, &d, &k, &c->comp, &bf16, &nofb, &sid, &c->device, &type, &dev, &str, &f[0],
+                          &f[1], &f[2], &f[3], &f[4], &f[5], &f[6]))
         return -1;
     c->ctx = reinterpret_cast<ds_ctx_t *>(ctx);
     c->n = n; c->d = d; c->k = k;
@@ -298,6 +375,8 @@ int init_calls(PyObject *self, PyObject *args, PyObject *)
     c->update = reinterpret_cast<UpdateFn>(f[2]);
     c->decode = reinterpret_cast<DecodeFn>(f[3]);
     c->server_update = reinterpret_cast<ServerUpdateFn>(f[4]);
+    c->ortho = reinterpret_cast<OrthoFn>(f[5]);
+    c->adamw = reinterpret_cast<AdamWFn>(f[6]);
     return 0;
 }
 
@@ -319,6 +398,8 @@ PyMethodDef methods[] = {
     {"server_update", fast(server_update), METH_FASTCALL, nullptr},
     {"update", fast(update), METH_FASTCALL, nullptr},
     {"decode", fast(decode), METH_FASTCALL, nullptr},
+    {"ortho", fast(ortho), METH_FASTCALL, nullptr},
+    {"adamw", fast(adamw), METH_FASTCALL, nullptr},
     {"close", close_calls, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

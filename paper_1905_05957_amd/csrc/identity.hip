@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kBlock) void k_identity_update(const float *q_in, f
 template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_identity_each(const float *q_in, int64_t d, Tail tail)
 {
-    const int64_t e = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    const int64_t e = tail.first() + threadIdx.x * 4;
     if (e >= d) return;
     const uint32_t f = tail.wants(e, d);
     if (f) tail.put(ld4_stream(q_in, e, d), e, d, f);
@@ -136,7 +136,7 @@ ds_status_t ds_identity_decode(ds_ctx *c, const ds_payload_t *p, int32_t row, fl
 template <class Tail>
 ds_status_t ds_identity_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
 {
-    k_identity_each<<<blocks4(c->cfg.d), kBlock, 0, st>>>(srv->dense, c->cfg.d, tail);
+    k_identity_each<<<static_cast<unsigned>(tail.n), kBlock, 0, st>>>(srv->dense, c->cfg.d, tail);
     return ds_launch_status();
 }
 template ds_status_t ds_identity_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);

@@ -261,10 +261,10 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // Direct copy of 16 bytes per lane, from `base` + `offset` into LDS at `lds` + 16 l for lane l; `base` and `lds` are the same for
 // the wavefront.  It has no output register.  Written as an instruction because the compiler waits for every
 // outstanding copy of its own builtin before the next read of LDS, also of another stage; the wait that is needed
-// stands in front of the barrier of that stage.
+// stands in front of the barrier of that stage.  m0 is a register the compiler does not allocate; nothing else here uses it.
 __device__ __forceinline__ void copy_to_lds(const char *base, uint32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory");
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void *p)
@@ -661,7 +661,7 @@ template <bool SPLIT>
 int64_t small_bytes(int64_t mp, int64_t np) { return (mp * np + mp * mp) * (SPLIT ? 4 : 2); }
 
 // Norm, operands, all steps and the result of one matrix, X [MP, np] and G (B in its place) in LDS.  Chains of small
-// dependent products are bound by latency: five steps on 96 x 64 took 15 launches and 54 us, 0 NEW us so.
+// dependent products are bound by latency: five steps on 96 x 64 took 15 launches and 54 us, 33 us so.
 //
 // Panels as in the large form; chunk c of row r of panel p lies at c ^ f(r, p), f = (r / 4) % 4, and with two halves the
 // panels take turns with hi and lo: 16 lanes that read rows, and 32 lanes that read transposing, meet different banks.
@@ -870,6 +870,8 @@ struct ds_ortho {
     const float *small_coef;
     double *partial;
     uint64_t *inside;                      // plane of bits: the elements of the matrices
+    const int32_t *vector_tiles[2];        // 2048-element tiles of the vector with an element outside, inside the matrices
+    int32_t n_vector_tiles[2];
     float *u;                              // [d] what is orthogonalised, where it is not m
     char *ws;
 };
@@ -1173,6 +1175,11 @@ ds_status_t run(const ds_ortho *o, const void *src, const Out &out, hipStream_t 
 }  // namespace
 
 const uint64_t *ds_ortho_inside(const ds_ortho *o) { return o->inside; }
+const int32_t *ds_ortho_tiles(const ds_ortho *o, bool inside, int32_t *n)
+{
+    *n = o->n_vector_tiles[inside];
+    return o->vector_tiles[inside];
+}
 int64_t ds_ortho_elements(const ds_ortho *o) { return o->cfg.d; }
 int ds_ortho_device(const ds_ortho *o) { return o->device; }
 bool ds_ortho_nesterov(const ds_ortho *o) { return (o->cfg.flags & DS_ORTHO_NESTEROV) != 0; }
@@ -1216,6 +1223,17 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
             for (int64_t r = 0; r < M.rows; ++r)
                 if (!mark(plane, M.offset + r * ld, M.offset + r * ld + M.cols)) return DS_ERR_CONFIG;
         }
+        std::vector<int32_t> vector_tiles[2];
+        for (int64_t first = 0; first < cfg->d; first += kTile) {
+            uint64_t any = 0, all = ~0ull;
+            for (int64_t e = first; e < std::min(first + kTile, cfg->d); e += 64) {
+                const uint64_t w = plane[static_cast<size_t>(e >> 6)];
+                any |= w;
+                all &= cfg->d - e >= 64 ? w : w | (~0ull << (cfg->d - e));
+            }
+            if (any) vector_tiles[1].push_back(static_cast<int32_t>(first / kTile));
+            if (~all) vector_tiles[0].push_back(static_cast<int32_t>(first / kTile));
+        }
         o = new ds_ortho();
         o->cfg = *cfg;
         o->cfg.mats = nullptr;
@@ -1247,6 +1265,7 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
                       at_inside = take(size_of(plane));
         int64_t at_small[3];
         for (int k = 0; k < 3; ++k) at_small[k] = take(size_of(t.small[k]));
+        const int64_t at_outside = take(size_of(vector_tiles[0])), at_within = take(size_of(vector_tiles[1]));
         const int64_t at_coef = take(size_of(o->coef));
         const int64_t at_partial = take(t.n_partial * 8), at_u = take(cfg->d * 4), at_sums = take(sum_bytes), at_ws = take(t.ws_bytes);
         ds_status_t rc = hipGetDevice(&o->device) == hipSuccess ? DS_OK : DS_ERR_DEVICE;
@@ -1263,6 +1282,12 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
             put(at_small[k], t.small[k]);
             o->small[k] = reinterpret_cast<const int32_t *>(base + at_small[k]);
             o->n_small[k] = static_cast<unsigned>(t.small[k].size());
+        }
+        put(at_outside, vector_tiles[0]);
+        put(at_within, vector_tiles[1]);
+        for (int k = 0; k < 2; ++k) {
+            o->vector_tiles[k] = reinterpret_cast<const int32_t *>(base + (k ? at_within : at_outside));
+            o->n_vector_tiles[k] = static_cast<int32_t>(vector_tiles[k].size());
         }
         put(at_coef, o->coef);
         o->small_coef = reinterpret_cast<const float *>(base + at_coef);

