@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kBlock) void k_ortho_norm(const Mat *__restrict__ m
 {
     __shared__ double lds[kWaves];
     const int2 pt = parts[blockIdx.x];
-    const Mat &M = mats[pt.x];
+    const Mat M = mats[pt.x];
     const int64_t total = static_cast<int64_t>(M.rows) * M.cols;
     const int64_t each = ((total + M.parts - 1) / M.parts + 3) & ~static_cast<int64_t>(3);
     const int64_t lo = each * pt.y, hi = lo + each < total ? lo + each : total;
@@ -181,10 +181,20 @@ __global__ __launch_bounds__(kBlock) void k_ortho_norm(const Mat *__restrict__ m
             s = fma(d, d, s);
         }
     } else {
-        for (int64_t t = lo + threadIdx.x; t < hi; t += kBlock) {
-            const uint32_t r = static_cast<uint32_t>(t) / static_cast<uint32_t>(M.cols);
-            const double v = load_flat<BF16>(src, M.offset + r * M.ld + (t - static_cast<int64_t>(r) * M.cols));
-            s = fma(v, v, s);
+        // column blocks: batches of eight elements asked for together
+        for (int64_t t0 = lo + threadIdx.x; t0 < hi; t0 += kBlock * 8) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t t = t0 + e * kBlock < hi ? t0 + e * kBlock : lo;     // no branch: one would wait for every load
+                const uint32_t r = static_cast<uint32_t>(t) / static_cast<uint32_t>(M.cols);
+                v[e] = load_flat<BF16>(src, M.offset + r * M.ld + (t - static_cast<int64_t>(r) * M.cols));
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (t0 + e * kBlock >= hi) v[e] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), s);
         }
     }
     s = block_sum(s, lds, false);
@@ -200,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_operands(const Mat *__restri
     __shared__ float tile[T][T + 1];
     __shared__ double sums[kThreads / 64];
     const Tile tl = tiles[blockIdx.x];
-    const Mat &M = mats[tl.mat];
+    const Mat M = mats[tl.mat];
     const int i0 = tl.i * T, j0 = tl.j * T;
     // the stored rows: four elements of one a thread, four rows
     const int row0 = M.flip ? j0 : i0, col0 = M.flip ? i0 : j0;
@@ -265,6 +275,15 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 __device__ __forceinline__ void copy_to_lds(const char *base, uint32_t offset, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory");
+}
+
+// The same address in every lane, as a scalar.
+__device__ __forceinline__ const char *uniform(const char *p)
+{
+    const uint64_t b = reinterpret_cast<uint64_t>(p);
+    const uint64_t lo = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b)));
+    const uint64_t hi = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b >> 32)));
+    return reinterpret_cast<const char *>(lo | (hi << 32));
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void *p)
@@ -366,8 +385,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
         }
     }
     const int64_t q_step = ACROSS ? PIECE : panel;
-    p_base += tl.k0 * panel;
-    q_base += tl.k0 * q_step;
+    p_base = uniform(p_base + tl.k0 * panel);
+    q_base = uniform(q_base + tl.k0 * q_step);
     const uint32_t lds_at = __builtin_amdgcn_readfirstlane(lds_address(lds)) + wave * 1024;
     auto copy = [&](int buffer) {
         const uint32_t to = lds_at + buffer * STAGE_BYTES;
@@ -617,7 +636,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_join(const Mat *__restrict__
 {
     constexpr int PER_TILE = SIDE * SIDE / 8 / kThreads;
     const Cut cut = cuts[blockIdx.x / PER_TILE];
-    const Mat &M = mats[cut.mat];
+    const Mat M = mats[cut.mat];
     const int t = (blockIdx.x % PER_TILE) * kThreads + threadIdx.x, row = t % SIDE, col = t / SIDE * 8;
     const int i = cut.i * SIDE + row, j = cut.j * SIDE + col;
     if (i >= M.mp || j >= (STAGE >= kApply ? M.np : M.mp)) return;
@@ -673,7 +692,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_small(const Mat *__restrict_
     constexpr int SQUARE = NB * (NB + 1) / 2, PER_WAVE = (SQUARE + WAVES - 1) / WAVES;
     __shared__ __attribute__((aligned(256))) char lds[CAP];
     __shared__ double sums[WAVES];
-    const Mat &M = mats[list[blockIdx.x]];
+    const Mat M = mats[list[blockIdx.x]];
     const int np = M.np, lane = lane_id(), wave = wave_id(), r = lane & 31, h = lane >> 5;
     char *G = lds, *X = lds + GBYTES;
     auto chunk = [&](char *base, int row, int panel, int c) {
@@ -733,10 +752,18 @@ __global__ __launch_bounds__(kThreads) void k_ortho_small(const Mat *__restrict_
 
     double s = 0.0;
     const uint32_t total = static_cast<uint32_t>(M.rows) * M.cols, cols = M.cols;
-    for (uint32_t t = threadIdx.x; t < total; t += kThreads) {
-        const uint32_t row = t / cols;
-        const double v = load_flat<BF16>(src, M.offset + row * M.ld + (t - row * cols));
-        s = fma(v, v, s);
+    for (uint32_t t0 = threadIdx.x; t0 < total; t0 += kThreads * 16) {       // sixteen elements asked for together
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const uint32_t t = t0 + e * kThreads < total ? t0 + e * kThreads : 0u, row = t / cols;     // no branch: one would wait
+            v[e] = load_flat<BF16>(src, M.offset + row * M.ld + (t - row * cols));
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (t0 + e * kThreads >= total) v[e] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), s);
     }
     s = wave_sum(s);
     if (lane == 0) sums[wave] = s;
@@ -746,17 +773,18 @@ __global__ __launch_bounds__(kThreads) void k_ortho_small(const Mat *__restrict_
     for (int w = 0; w < WAVES; ++w) s += sums[w];
     const double norm = sqrt(s) + static_cast<double>(eps);
     const double inv = norm == 0.0 ? 0.0 : static_cast<double>(M.scale) / norm;
+#pragma unroll 4
     for (int t = threadIdx.x; t < MP * np / 8; t += kThreads) {
         const int i = M.flip ? t % MP : t / (np / 8), j = (M.flip ? t / MP : t % (np / 8)) * 8;
         float v[8];
+        const int64_t row = M.offset + (M.flip ? i : i * M.ld), step = M.flip ? M.ld : 1;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[e] = 0.f;
-            if (i < M.m && j + e < M.n) {
-                const int64_t at = M.offset + (M.flip ? (j + e) * M.ld + i : i * M.ld + j + e);
-                v[e] = static_cast<float>(static_cast<double>(load_flat<BF16>(src, at)) * inv);
-            }
+        for (int e = 0; e < 8; ++e) {                          // no branch here either
+            const int64_t at = row + (j + e) * step;
+            v[e] = load_flat<BF16>(src, i < M.m & j + e < M.n ? at : M.offset);
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = i < M.m & j + e < M.n ? static_cast<float>(static_cast<double>(v[e]) * inv) : 0.f;
         put8(X, i, j, v);
     }
     __syncthreads();
@@ -776,7 +804,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_small(const Mat *__restrict_
                 for (int e = 0; e < 16; ++e) acc[u][e] = 0.f;
                 char *from = STAGE == kGram ? X : G;
                 const int panels = (STAGE == kGram ? np : MP) / K;
-#pragma unroll 2
+#pragma unroll 4
                 for (int p = 0; p < panels; ++p) {
                     const half8 fp[2] = {rows(from, bi * 32, p, 0), rows(from, bi * 32, p, 1)};
                     const half8 fq[2] = {rows(from, bj * 32, p, 0), rows(from, bj * 32, p, 1)};
