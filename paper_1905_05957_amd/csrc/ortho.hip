@@ -349,24 +349,25 @@ __device__ __forceinline__ void wait_copies()       // at most N copies of this 
 // of k as well; Q = X, in the last product, lies with k across the rows: its tile is transposed on the way from LDS to the
 // registers.
 //
-// Pipeline.  LDS holds S stages of 16 (32) values of k.  While stage k is multiplied from registers, the fragments of stage k
-// + 1 are read from LDS and the copies of stages k + 2 .. k + S, which pass no registers, are under way; one barrier a stage.
+// Pipeline.  LDS holds S stages of G panels, of 16 (32) values of k each.  While a panel is multiplied from registers, the
+// fragments of the next are read from LDS and the copies of the stages behind, which pass no registers, are under way; one
+// barrier a stage.  (Small tiles, whose panels are a few instructions, take two panels a stage.)
 //
 // LDS has 64 banks, 256 bytes.  A copy fills it linearly, so what a lane copies is chosen such that the 16-byte chunk c of
 // row r lies at c ^ f(r), and 16 lanes that read 16 rows of one chunk (or, transposing, 32 lanes 4 rows of 4 chunks) meet
 // different banks: 267 and 228 bytes a clock measured, 43 and 80 without.
 //
 // The wavefront multiplies Q' P': a lane then holds a row i of C and four consecutive j at a time.
-template <int TM, int TN, int WM, int WN, int S, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
+template <int TM, int TN, int WM, int WN, int S, int G, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
 __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Mat *__restrict__ mats, const Tile *__restrict__ tiles,
                                                                              char *ws, float *parts, Step step, Out out)
 {
     constexpr int WAVES_N = TN / WN, WAVES = (TM / WM) * WAVES_N, FM = WM / 32, FN = WN / 32;
     constexpr bool ACROSS = STAGE >= kApply;                   // Q is X
     constexpr int K = kPanel<SPLIT>, PIECE = K * kRow;         // values of k in a stage; a panel's part of a stage of X
-    constexpr int PBYTES = TM * kRow, QBYTES = TN * kRow, STAGE_BYTES = PBYTES + QBYTES;
-    constexpr int PCOPIES = PBYTES / (WAVES * 1024), QCOPIES = QBYTES / (WAVES * 1024), COPIES = PCOPIES + QCOPIES;
-    static_assert(PCOPIES * WAVES * 1024 == PBYTES && QCOPIES * WAVES * 1024 == QBYTES && S >= 3, "tile");
+    constexpr int PBYTES = TM * kRow, QBYTES = TN * kRow, PANEL_BYTES = PBYTES + QBYTES, STAGE_BYTES = G * PANEL_BYTES;
+    constexpr int PCOPIES = PBYTES / (WAVES * 1024), QCOPIES = QBYTES / (WAVES * 1024), COPIES = G * (PCOPIES + QCOPIES);
+    static_assert(PCOPIES * WAVES * 1024 == PBYTES && QCOPIES * WAVES * 1024 == QBYTES && (S == 3 || S == 4) && (G == 1 || G == 2), "tile");
     __shared__ __attribute__((aligned(256))) char lds[S * STAGE_BYTES];
     const Tile tl = tiles[blockIdx.x];
     const Mat &M = mats[tl.mat];
@@ -374,7 +375,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int wi = (wave / WAVES_N) * WM, wj = (wave % WAVES_N) * WN;
     const int64_t panel = M.panel;
-    const int stages = tl.k1 - tl.k0;                          // even: rounded sizes are multiples of 64
+    const int stages = (tl.k1 - tl.k0) / G;                    // panels come in even numbers: rounded sizes are multiples of 64
     const char *X = ws + M.x[step.from];
     const char *P = STAGE == kGram ? X : ws + (STAGE == kPoly ? M.g : M.b);
     const char *Q = ACROSS ? X : P;
@@ -403,13 +404,16 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     q_base = uniform(q_base + tl.k0 * q_step);
     const uint32_t lds_at = __builtin_amdgcn_readfirstlane(lds_address(lds)) + wave * 1024;
     auto copy = [&](int buffer) {
-        const uint32_t to = lds_at + buffer * STAGE_BYTES;
 #pragma unroll
-        for (int t = 0; t < PCOPIES; ++t) copy_to_lds(p_base, pa[t], to + t * WAVES * 1024);
+        for (int g = 0; g < G; ++g) {
+            const uint32_t to = lds_at + buffer * STAGE_BYTES + g * PANEL_BYTES;
 #pragma unroll
-        for (int t = 0; t < QCOPIES; ++t) copy_to_lds(q_base, qa[t], to + PBYTES + t * WAVES * 1024);
-        p_base += panel;
-        q_base += q_step;
+            for (int t = 0; t < PCOPIES; ++t) copy_to_lds(p_base, pa[t], to + t * WAVES * 1024);
+#pragma unroll
+            for (int t = 0; t < QCOPIES; ++t) copy_to_lds(q_base, qa[t], to + PBYTES + t * WAVES * 1024);
+            p_base += panel;
+            q_base += q_step;
+        }
     };
     // Fragments of 32 rows by 16 values: lane l holds row l % 32, values 8 (l / 32) .. + 7.  Two of them in a stage, q: hi and
     // lo, or the two halves of k.
@@ -425,8 +429,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
         // split: group g of 16 columns is a panel of its own, hi or lo a half of its rows; one half: a half of the panel's rows
         col_at[q] = SPLIT ? g * PIECE + k * kRow + ((q ^ g) * 32) + byte : (q * 16 + k) * kRow + g * 32 + byte;
     }
-    auto read = [&](Frags &f, int buffer) {
-        const char *lp = lds + buffer * STAGE_BYTES + wi * kRow, *lq = lds + buffer * STAGE_BYTES + PBYTES + wj * kRow;
+    auto read = [&](Frags &f, int buffer, int g) {
+        const char *lp = lds + buffer * STAGE_BYTES + g * PANEL_BYTES + wi * kRow, *lq = lp + PBYTES + (wj - wi) * kRow;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
 #pragma unroll
@@ -476,25 +480,13 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     else wait_copies<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
-    read(f0, 0);
+    read(f0, 0, 0);
     int here = 0;                                          // buffer of stage k
-    // Stage k from `now`, stage k + 1 into `next`; steady: as many stages follow as there are buffers.  The last stage
-    // stands by itself, so that on every way to a multiplication the reads of the next fragments come after those of its
-    // own: where the two ways met, the compiler waited for all of them.
-    auto one_stage = [&](auto steady, int k, Frags &now, Frags &next) {
-        const int under_way = stages - 2 - k;              // stages after the next that have been asked for
-        if (decltype(steady)::value || under_way >= S - 2) wait_copies<(S - 2) * COPIES>();
-        else if (S > 3 && under_way == S - 3) wait_copies<(S - 3) * COPIES>();
-        else if (S > 4 && under_way == S - 4) wait_copies<(S - 4) * COPIES>();
-        else wait_copies<0>();
-        // everybody's copies of stage k + 1 are there, and everybody holds stage k in registers
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" : : : "memory");
-        if (decltype(steady)::value || k + S < stages) copy(here);
-        here = here + 1 == S ? 0 : here + 1;
-        // nothing of this crosses a barrier, and the reads are spread over the first products
+    // The next panel's fragments are read while this one's are multiplied: the reads are spread over the first products, and
+    // nothing of it crosses a barrier.
+    auto read_and_multiply = [&](const Frags &now, Frags &next, int g) {
         __builtin_amdgcn_sched_barrier(0);
-        read(next, here);
+        read(next, here, g);
         multiply(now);
 #pragma unroll
         for (int t = 0; t < 2 * (FM + (ACROSS ? 2 : 1) * FN); ++t) {
@@ -503,16 +495,43 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
         }
         __builtin_amdgcn_sched_barrier(0);
     };
+    // The last panel of stage k from `now`, the first of stage k + 1 into `next`; steady: as many stages follow as there are
+    // buffers.  The last panel of all stands by itself, so that on every way to a multiplication the reads of the next
+    // fragments come after those of its own: where the two ways met, the compiler waited for all of them.
+    auto cross = [&](auto steady, int k, const Frags &now, Frags &next) {
+        const int under_way = stages - 2 - k;              // stages after the next that have been asked for
+        if (decltype(steady)::value || under_way >= S - 2) wait_copies<(S - 2) * COPIES>();
+        else if (S > 3 && under_way == S - 3) wait_copies<(S - 3) * COPIES>();
+        else wait_copies<0>();
+        // everybody's copies of stage k + 1 are there, and everybody holds the end of stage k in registers
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
+        if (decltype(steady)::value || k + S < stages) copy(here);
+        here = here + 1 == S ? 0 : here + 1;
+        read_and_multiply(now, next, 0);
+    };
     int k = 0;
-    for (; k + 1 + S < stages; k += 2) {
-        one_stage(std::true_type{}, k, f0, f1);
-        one_stage(std::true_type{}, k + 1, f1, f0);
+    if constexpr (G == 2) {
+        for (; k + S < stages; ++k) {
+            read_and_multiply(f0, f1, 1);
+            cross(std::true_type{}, k, f1, f0);
+        }
+        for (; k + 1 < stages; ++k) {
+            read_and_multiply(f0, f1, 1);
+            cross(std::false_type{}, k, f1, f0);
+        }
+        read_and_multiply(f0, f1, 1);
+    } else {
+        for (; k + 1 + S < stages; k += 2) {
+            cross(std::true_type{}, k, f0, f1);
+            cross(std::true_type{}, k + 1, f1, f0);
+        }
+        for (; k + 2 < stages; k += 2) {
+            cross(std::false_type{}, k, f0, f1);
+            cross(std::false_type{}, k + 1, f1, f0);
+        }
+        cross(std::false_type{}, k, f0, f1);
     }
-    for (; k + 2 < stages; k += 2) {
-        one_stage(std::false_type{}, k, f0, f1);
-        one_stage(std::false_type{}, k + 1, f1, f0);
-    }
-    one_stage(std::false_type{}, k, f0, f1);
     multiply(f1);
 
     if (tl.slot >= 0) {
@@ -1007,13 +1026,16 @@ std::vector<Tile> by_xcd(const std::vector<Tile> &list)
     return out;
 }
 
-// What a launch of these tiles takes, in microseconds, from times measured with 1 to 4096 tiles of 16 to 512 stages.  A
-// workgroup takes `base` (addresses, first copies, results) and a time per stage, which grow with the workgroups per
-// compute unit (c): alone and with the device full a stage of a 256 x 256 tile takes 0.75 and 1.25 us (0.55 and 0.95 with one half; 32 values of k then), of a 128 x 128
-// tile 0.25 and, two per compute unit, 0.68 (0.19, 0.53), of a 64 x 64 tile 0.16 and, four, 0.48 (0.13, 0.45).
+// What a launch of these tiles takes, in microseconds, from times measured with 1 to 4096 tiles of 8 to 512 panels.  A
+// workgroup takes `base` (addresses, first copies, results) and a time per panel, which grow with the workgroups per compute
+// unit (c): alone and with the device full a panel of a 256 x 256 tile takes 0.75 and 1.25 us (0.55 and 0.95 with one half;
+// 32 values of k then), of a 128 x 128 tile 0.25 and, two per compute unit, 0.68 (0.19, 0.53), of a 64 x 64 tile 0.11 and,
+// two, 0.25 (0.09, 0.22).
+int tiles_at_once(int side) { return side == 256 ? 256 : 512; }
+
 double launch_time(const std::vector<Tile> &tiles, int side, bool split)
 {
-    const size_t at_once = side == 256 ? 256 : side == 128 ? 512 : 1024;
+    const size_t at_once = static_cast<size_t>(tiles_at_once(side));
     double time = 0.0;
     for (size_t first = 0; first < tiles.size(); first += at_once) {
         const size_t end = std::min(first + at_once, tiles.size());
@@ -1023,11 +1045,11 @@ double launch_time(const std::vector<Tile> &tiles, int side, bool split)
             longest = std::max<int64_t>(longest, tiles[k].k1 - tiles[k].k0);
             sum += tiles[k].k1 - tiles[k].k0;
         }
-        const double stage = side == 256 ? (split ? 0.75 + 0.5 * c : 0.55 + 0.4 * c)
-                             : side == 128 ? (c <= 1.0 ? 0.06 * c + (split ? 0.25 : 0.19) : (split ? 0.31 + 0.37 * (c - 1.0) : 0.25 + 0.28 * (c - 1.0)))
-                                           : 0.08 * c + (split ? 0.16 : 0.13);
-        const double more = std::max(c - 1.0, 0.0);
-        const double base = side == 256 ? (split ? 13.0 : 7.0) : side == 128 ? 4.5 + (split ? 7.5 : 3.5) * more : 2.2 + (split ? 1.2 : 0.3) * more;
+        const double more = std::max(c - 1.0, 0.0), one = std::min(c, 1.0);
+        const double stage = side == 256   ? (split ? 0.75 + 0.5 * c : 0.55 + 0.4 * c)
+                             : side == 128 ? (split ? 0.25 + 0.06 * one + 0.37 * more : 0.19 + 0.06 * one + 0.28 * more)
+                                           : (split ? 0.10 + 0.035 * one + 0.11 * more : 0.09 + 0.02 * one + 0.11 * more);
+        const double base = side == 256 ? (split ? 13.0 : 7.0) : side == 128 ? 4.5 + (split ? 7.5 : 3.5) * more : 2.8;
         // rounds run into each other: only the last one's longest sum counts in full
         time += base + stage * (end == tiles.size() ? static_cast<double>(longest) : static_cast<double>(sum) / static_cast<double>(end - first));
     }
@@ -1040,7 +1062,7 @@ double launch_time(const std::vector<Tile> &tiles, int side, bool split)
 void deal_out(const std::vector<Tile> &list, int side, bool cutting, Work &w)
 {
     constexpr int kLeast = 8;              // stages of a part: below, filling the pipeline costs more than it saves
-    const int at_once = side == 256 ? 256 : side == 128 ? 512 : 1024;
+    const int at_once = tiles_at_once(side);
     w.side = side;
     std::vector<Tile> whole, cut, pieces;
     int64_t total = 0, cut_stages = 0;
@@ -1163,7 +1185,7 @@ template <int SIDE, bool SPLIT, int STAGE, int OUT>
 void product_of(const ds_ortho *o, const ds_ortho::Launch &l, const Step &s, const Out &out, hipStream_t st)
 {
     constexpr int WM = SIDE == 64 ? 32 : SIDE == 128 ? 64 : 128, WN = SIDE == 64 ? 32 : 64, THREADS = (SIDE / WM) * (SIDE / WN) * 64;
-    k_ortho_product<SIDE, SIDE, WM, WN, 4, SPLIT, STAGE, OUT><<<l.n_tiles, THREADS, 0, st>>>(o->mats, l.tiles, o->ws, o->sums, s, out);
+    k_ortho_product<SIDE, SIDE, WM, WN, 4, SIDE == 64 ? 2 : 1, SPLIT, STAGE, OUT><<<l.n_tiles, THREADS, 0, st>>>(o->mats, l.tiles, o->ws, o->sums, s, out);
     if (l.n_cuts)
         k_ortho_join<SIDE, SPLIT, STAGE, OUT><<<l.n_cuts * (SIDE * SIDE / 8 / kThreads), kThreads, 0, st>>>(o->mats, l.cuts, o->ws, o->sums, s,
                                                                                                          out);
