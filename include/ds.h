@@ -288,10 +288,12 @@ ds_status_t ds_server_aggregate_compress_update(ds_ctx_t *ctx, uint64_t step, co
  * element may belong to two of them.  Elements in no matrix are not read and not written.
  *
  * Products: operands are held as the sum of two halves of 11 bits (three matrix products, sums in fp32), so results are
- * as those of fp32 products; with DS_ORTHO_HALF as one half of 11 bits (one product, a third of the time), for results that
- * are kept in bf16 or need no more.  Both are scaled by powers of two, so small entries keep their bits.  Norms are
- * summed in fp64.  The iteration must not let singular values grow beyond 2: every list of coefficients that
- * converges for singular values in [0, 1] does not.  Sums are taken in a fixed order: equal calls give equal bits. */
+ * as those of fp32 products; with DS_ORTHO_HALF as one half of 11 bits (one product, a third of the arithmetic), for results
+ * that are kept in bf16 or need no more.  They are scaled by powers of two, so small entries keep their bits.  Norms are
+ * summed in fp64.  Range: singular values must stay below 2, which those of every list that converges for singular values
+ * in [0, 1] do, and b t + c t^2 and a + b t + c t^2 within 15 for t in [0, 1] (else DS_ERR_CONFIG).  Sums are taken in a
+ * fixed order: equal calls on equal plans give equal bits.  What is not finite stays in its matrix.
+ */
 typedef struct {
     int64_t offset;           /* of element (0, 0) in the vector */
     int64_t ld;               /* elements between rows, >= cols (0: cols) */
@@ -324,7 +326,7 @@ typedef struct ds_ortho ds_ortho_t;
 
 /* Creates a plan on the current device with its tables and its workspace (4 bytes per element of the vector and about 12 per
  * element of the matrices, half of that with DS_ORTHO_HALF, each matrix's sides rounded up to the tiles of its kernels).  Errors: NULL, SHAPE (d, n_mats, steps or a matrix out of range), CONFIG (bad
- * enum or flag, eps or a coefficient negative or not finite where it must not be, two matrices that share an element), DEVICE.
+ * enum or flag, eps negative or not finite, coefficients out of range, two matrices that share an element), DEVICE (memory).
  * Calls with one plan share its workspace: they must not overlap (one stream, or ordered by events; that holds for
  * replays of captured graphs too). */
 ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out);

@@ -21,9 +21,8 @@
 #include "ds_internal.h"
 #include "tails.h"
 
-#include <math.h>
-
 #include <algorithm>
+#include <cmath>
 #include <new>
 #include <type_traits>
 #include <vector>
@@ -1236,6 +1235,19 @@ ds_status_t run(const ds_ortho *o, const void *src, const Out &out, hipStream_t 
     return o->split ? run<true, SRC_BF16, OUT>(o, src, out, st) : run<false, SRC_BF16, OUT>(o, src, out, st);
 }
 
+// B and, with two halves, B + a are held times kPolyScale: b t + c t^2 and a + b t + c t^2 must stay below 16 for the squared
+// singular values t, [0, 1] here; 15 leaves room for those that a step takes somewhat beyond 1.
+bool coefficients_fit(const float *q)
+{
+    const double a = q[0], b = q[1], c = q[2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    double ends[3] = {0.0, 1.0, 0.0};
+    if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < 1.0) ends[2] = -b / (2.0 * c);
+    for (double t : ends)
+        if (std::fabs(b * t + c * t * t) > 15.0 || std::fabs(a + b * t + c * t * t) > 15.0) return false;
+    return true;
+}
+
 }  // namespace
 
 const uint64_t *ds_ortho_inside(const ds_ortho *o) { return o->inside; }
@@ -1268,8 +1280,8 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
     if (cfg->factor < DS_ORTHO_FACTOR_NONE || cfg->factor > DS_ORTHO_FACTOR_RMS) return DS_ERR_CONFIG;
     if (cfg->flags & ~(DS_ORTHO_NESTEROV | DS_ORTHO_HALF)) return DS_ERR_CONFIG;
     if (cfg->coef)
-        for (int32_t k = 0; k < 3 * cfg->steps; ++k)
-            if (!std::isfinite(cfg->coef[k])) return DS_ERR_CONFIG;
+        for (int32_t k = 0; k < cfg->steps; ++k)
+            if (!coefficients_fit(cfg->coef + 3 * k)) return DS_ERR_CONFIG;
     for (int32_t k = 0; k < cfg->n_mats; ++k) {
         const ds_matrix_t &M = cfg->mats[k];
         if (M.rows < 1 || M.cols < 1 || M.offset < 0 || std::min(M.rows, M.cols) > 32768 || std::max(M.rows, M.cols) > (1 << 24)) return DS_ERR_SHAPE;

@@ -433,3 +433,40 @@ def test_refusals_on_the_device(gpu_device):
     assert torch.equal(x, before[0]) and torch.equal(m, before[1])
     for p in (plan, other, ctx):
         p.close()
+
+
+def test_the_longest_vector(gpu_device):
+    """d = 2^31 - 1: offsets past 2^32 bytes, in a bf16 vector, in the model and in the passes over the message."""
+    d = 2 ** 31 - 1
+    mats = [(0, 33, 65), (d - 300 * 500 - 7, 300, 500), (2 ** 30 + 1, 40, 30, 50)]
+    plan = P.OrthoPlan(d, mats)
+    src = torch.zeros(d, dtype=torch.bfloat16, device=gpu_device)
+    for k, m in enumerate(mats):
+        view(src, m).copy_(random_flat(m[1] * m[2], gpu_device, 70 + k).view(m[1], m[2]))
+    dst = torch.zeros_like(src)
+    plan.orthogonalize(src, dst)
+    for m in mats:
+        check(view(dst, m), reference(view(src, m)), False)
+    assert not dst[2145:2 ** 30].any() and not dst[d - 7:].any()
+    del src, dst
+    ctx = P.Context("sign", 1, d, scale_mode="chunk", chunk=2048)
+    ps = ctx.alloc_payload(1)
+    ps.scales.fill_(2.0)
+    ps.sign_words[:, -1] = 5                              # elements d - 63 and d - 61
+    x = torch.zeros(d, device=gpu_device)
+    v = torch.zeros(d, device=gpu_device)
+    m1 = torch.zeros(d, device=gpu_device)
+    # the message's other words are zero: every element is +2
+    ctx.apply_update_ortho(plan, ps, x, m1, 0.5, 0.5)
+    for m in mats:
+        q = torch.full((m[1], m[2]), 2.0, device=gpu_device, dtype=torch.float64)
+        if m[0] + (m[1] - 1) * m[2] + m[2] > d - 63:
+            flat = torch.arange(m[0], m[0] + m[1] * m[2], device=gpu_device).view(m[1], m[2])
+            q[(flat == d - 63) | (flat == d - 61)] = -2.0
+        assert torch.equal(view(m1, m).double(), q)
+        want = -0.5 * reference(q)
+        assert (view(x, m).double() - want).abs().max() <= 903 * 16 * 2.0 ** -22 * want.abs().max() + 2.0 ** -23
+    ctx.apply_update_adamw(ps, 0, x, m1, v, 0.25, skip=plan)
+    assert float(v[-1]) > 0 and float(x[-1]) < 0 and float(x[d - 3]) < 0 and not view(v, mats[1]).any()
+    plan.close()
+    ctx.close()

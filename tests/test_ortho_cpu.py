@@ -42,6 +42,11 @@ def test_create_refuses_what_it_cannot_take():
     assert _create(factor=-1) == CONFIG and _create(factor=3) == CONFIG
     assert _create(flags=4) == CONFIG and _create(flags=-1) == CONFIG
     assert _create(steps=1, coef=[1.5, float("nan"), 0.0]) == CONFIG
+    # the polynomial leaves the range in which B is held: at an end, in between, in the second step
+    assert _create(steps=1, coef=[16.0, 0.0, 0.0]) == CONFIG and _create(steps=1, coef=[1.0, 20.0, 0.0]) == CONFIG
+    assert _create(steps=1, coef=[1.0, 70.0, -70.0]) == CONFIG
+    assert _create(steps=2, coef=[1.5, -0.5, 0.0, 1.0, -17.0, 0.0]) == CONFIG
+    assert _create(steps=1, coef=[8.2872, -23.5959, 17.3004]) in (0, DEVICE)
 
 
 @pytest.mark.parametrize("mat", [
