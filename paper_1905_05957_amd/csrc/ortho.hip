@@ -58,8 +58,10 @@ struct Mat {
 
 // What a workgroup of a product takes: tile (i, j) of a matrix, stages [k0, k1) of its sum.  slot < 0: the whole sum; else this
 // part goes to that slot of the parts' buffer and a launch behind the product puts the parts together.
+// The matrix stands in it: a number of one would cost a second trip to memory before the first copy.
 struct Tile {
-    int32_t mat, i, j, k0, k1, slot, pad_[2];
+    int32_t mat, i, j, k0, k1, slot;
+    Mat m;
 };
 
 struct Cut {                     // a tile in parts
@@ -202,14 +204,13 @@ __global__ __launch_bounds__(kBlock) void k_ortho_norm(const Mat *__restrict__ m
 
 // X = U / (norm + eps), times 2^s, zero beyond the matrix.
 template <bool SPLIT, bool BF16>
-__global__ __launch_bounds__(kThreads) void k_ortho_operands(const Mat *__restrict__ mats, const Tile *__restrict__ tiles,
-                                                             const void *src, const double *__restrict__ partial, float eps, char *ws)
+__global__ __launch_bounds__(kThreads) void k_ortho_operands(const Tile *__restrict__ tiles, const void *src, const double *__restrict__ partial, float eps, char *ws)
 {
     constexpr int T = 64;
     __shared__ float tile[T][T + 1];
     __shared__ double sums[kThreads / 64];
-    const Tile tl = tiles[blockIdx.x];
-    const Mat M = mats[tl.mat];
+    const Tile &tl = tiles[blockIdx.x];
+    const Mat &M = tl.m;
     const int i0 = tl.i * T, j0 = tl.j * T;
     // the stored rows: four elements of one a thread, four rows
     const int row0 = M.flip ? j0 : i0, col0 = M.flip ? i0 : j0;
@@ -306,20 +307,21 @@ __device__ __forceinline__ float product_scale(const Mat &M, const Step &step)
 template <int STAGE>
 __device__ __forceinline__ float old_scale(const Step &step)
 {
-    return STAGE == kGram ? 0.f : STAGE == kPoly ? step.b * (kPolyScale / kGramScale) : step.a;
+    return STAGE == kPoly ? step.b * (kPolyScale / kGramScale) : 0.f;
 }
 
-// With two halves a lies on B's diagonal, rounded as X is, and the last product does not read X a second time (340 MB less
-// for sixty matrices of 85 M elements).  With one half a keeps its 24 bits and is applied to X itself.
-template <bool SPLIT, int STAGE>
-constexpr bool kReadsOld = STAGE == kPoly || (STAGE >= kApply && !SPLIT);
+// a lies on B's diagonal, rounded as B is, so the last product does not read X a second time.  With one half that rounding is
+// 2^-11 of a row at most, as X's own is; results in bf16 lie 1.9e-3 (root mean square, relative) from those in 64 bits with
+// it and 2.0e-3 with a applied to X in fp32; rounding to bf16 alone is 1.66e-3.
+template <int STAGE>
+constexpr bool kReadsOld = STAGE == kPoly;
 
 // One element of a result from its product and the old value.
-template <bool SPLIT, int STAGE>
+template <int STAGE>
 __device__ __forceinline__ float result(float alpha, float beta, const Step &step, float product, float old, bool diagonal)
 {
-    float v = kReadsOld<SPLIT, STAGE> ? __fmaf_rn(beta, old, product * alpha) : product * alpha;
-    if (SPLIT && STAGE == kPoly && diagonal) v = __fmaf_rn(step.a, kPolyScale, v);
+    float v = kReadsOld<STAGE> ? __fmaf_rn(beta, old, product * alpha) : product * alpha;
+    if (STAGE == kPoly && diagonal) v = __fmaf_rn(step.a, kPolyScale, v);
     return v;
 }
 
@@ -358,8 +360,7 @@ __device__ __forceinline__ void wait_copies()       // at most N copies of this 
 //
 // The wavefront multiplies Q' P': a lane then holds a row i of C and four consecutive j at a time.
 template <int TM, int TN, int WM, int WN, int S, int G, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
-__global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Mat *__restrict__ mats, const Tile *__restrict__ tiles,
-                                                                             char *ws, float *parts, Step step, Out out)
+__global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Tile *__restrict__ tiles, char *ws, float *parts, Step step, Out out)
 {
     constexpr int WAVES_N = TN / WN, WAVES = (TM / WM) * WAVES_N, FM = WM / 32, FN = WN / 32;
     constexpr bool ACROSS = STAGE >= kApply;                   // Q is X
@@ -368,8 +369,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     constexpr int PCOPIES = PBYTES / (WAVES * 1024), QCOPIES = QBYTES / (WAVES * 1024), COPIES = G * (PCOPIES + QCOPIES);
     static_assert(PCOPIES * WAVES * 1024 == PBYTES && QCOPIES * WAVES * 1024 == QBYTES && (S == 3 || S == 4) && (G == 1 || G == 2), "tile");
     __shared__ __attribute__((aligned(256))) char lds[S * STAGE_BYTES];
-    const Tile tl = tiles[blockIdx.x];
-    const Mat &M = mats[tl.mat];
+    const Tile &tl = tiles[blockIdx.x];
+    const Mat &M = tl.m;
     const int i0 = tl.i * TM, j0 = tl.j * TN, mp = M.mp, np = M.np;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int wi = (wave / WAVES_N) * WM, wj = (wave % WAVES_N) * WN;
@@ -551,7 +552,6 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     }
     const float alpha = product_scale<STAGE>(M, step), beta = old_scale<STAGE>(step);
     const int j_end = ACROSS ? np : mp;
-    const char *old = STAGE == kPoly ? P : X;
     char *to = ws + (STAGE == kGram ? M.g : STAGE == kPoly ? M.b : M.x[1 - step.from]);
     // the last product goes into the vector along its rows, through LDS: a region of its own for every wavefront
     constexpr int PITCH = WN + 1;
@@ -587,12 +587,12 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
             }
         }
         Eight<SPLIT> was[FN][2];                               // asked for together
-        if (kReadsOld<SPLIT, STAGE>) {
+        if (kReadsOld<STAGE>) {
 #pragma unroll
             for (int b = 0; b < FN; ++b)
 #pragma unroll
                 for (int g = 0; g < 2; ++g)
-                    if (j0 + wj + b * 32 < j_end) was[b][g].load(old + element_at<SPLIT>(panel, ib + r, j0 + wj + b * 32 + 16 * g + 8 * h));
+                    if (j0 + wj + b * 32 < j_end) was[b][g].load(P + element_at<SPLIT>(panel, ib + r, j0 + wj + b * 32 + 16 * g + 8 * h));
         }
 #pragma unroll
         for (int b = 0; b < FN; ++b) {
@@ -604,9 +604,9 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
                 float v[8], x[8];
                 const int i = ib + r, j = jb + 16 * g + 8 * h;
                 const int64_t at = element_at<SPLIT>(panel, i, j);
-                if (kReadsOld<SPLIT, STAGE>) was[b][g].values(x);
+                if (kReadsOld<STAGE>) was[b][g].values(x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = result<SPLIT, STAGE>(alpha, beta, step, c.v[e], x[e], i == j + e);
+                for (int e = 0; e < 8; ++e) v[e] = result<STAGE>(alpha, beta, step, c.v[e], x[e], i == j + e);
                 if constexpr (STAGE != kLast) {
                     store8<SPLIT>(to + at, v);
                     if (STAGE < kApply && tl.i != tl.j) {
@@ -683,13 +683,13 @@ __global__ __launch_bounds__(kThreads) void k_ortho_join(const Mat *__restrict__
     const float alpha = product_scale<STAGE>(M, step), beta = old_scale<STAGE>(step);
     const int64_t at = element_at<SPLIT>(M.panel, i, j);
     float v[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w}, x[8];
-    if (kReadsOld<SPLIT, STAGE>) {
+    if (kReadsOld<STAGE>) {
         Eight<SPLIT> was;
-        was.load(ws + (STAGE == kPoly ? M.g : M.x[step.from]) + at);
+        was.load(ws + M.g + at);
         was.values(x);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = result<SPLIT, STAGE>(alpha, beta, step, v[e], x[e], i == j + e);
+    for (int e = 0; e < 8; ++e) v[e] = result<STAGE>(alpha, beta, step, v[e], x[e], i == j + e);
     if constexpr (STAGE != kLast) {
         char *to = ws + (STAGE == kGram ? M.g : STAGE == kPoly ? M.b : M.x[1 - step.from]);
         store8<SPLIT>(to + at, v);
@@ -856,7 +856,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_small(const Mat *__restrict_
                     float v[8];
                     if (STAGE == kPoly) get8(G, i, j, v);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = STAGE == kGram ? c.v[e] * alpha : __fmaf_rn(beta, v[e], c.v[e] * alpha);
+                    for (int e = 0; e < 8; ++e) v[e] = result<STAGE>(alpha, beta, step, c.v[e], v[e], i == j + e);
                     put8(G, i, j, v);
                     if (bi != bj)
 #pragma unroll
@@ -868,7 +868,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_small(const Mat *__restrict_
         square(std::integral_constant<int, kGram>{});
         square(std::integral_constant<int, kPoly>{});
         // X <- a X + B X: a wavefront's columns are its own, so X changes in place
-        const float alpha = product_scale<kApply>(M, step), beta = step.a;
+        const float alpha = product_scale<kApply>(M, step);
         for (int bj = wave; bj < np / 32; bj += WAVES) {
             f32x16 acc[NB];
 #pragma unroll
@@ -890,9 +890,8 @@ __global__ __launch_bounds__(kThreads) void k_ortho_small(const Mat *__restrict_
                     const EightColumns c(acc[b], g);
                     const int i = b * 32 + r, j = bj * 32 + 16 * g + 8 * h;
                     float v[8];
-                    get8(X, i, j, v);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn(beta, v[e], c.v[e] * alpha);
+                    for (int e = 0; e < 8; ++e) v[e] = c.v[e] * alpha;
                     if (k + 1 < steps) put8(X, i, j, v);
                     else eight_into_vector<OUT>(M, out, i, j, v);
                 }
@@ -997,7 +996,7 @@ std::vector<Tile> list_tiles(const std::vector<Mat> &mats, int side, int stage, 
         for (int32_t i0 = 0; i0 < ti; i0 += strip)
             for (int32_t j = 0; j < tj; ++j)
                 for (int32_t i = i0; i < std::min(i0 + strip, ti); ++i)
-                    if (!square || j <= i) list.push_back(Tile{k, i, j, 0, length(k) / panel, -1, {0, 0}});
+                    if (!square || j <= i) list.push_back(Tile{k, i, j, 0, length(k) / panel, -1, mats[static_cast<size_t>(k)]});
     }
     return list;
 }
@@ -1184,7 +1183,7 @@ template <int SIDE, bool SPLIT, int STAGE, int OUT>
 void product_of(const ds_ortho *o, const ds_ortho::Launch &l, const Step &s, const Out &out, hipStream_t st)
 {
     constexpr int WM = SIDE == 64 ? 32 : SIDE == 128 ? 64 : 128, WN = SIDE == 64 ? 32 : 64, THREADS = (SIDE / WM) * (SIDE / WN) * 64;
-    k_ortho_product<SIDE, SIDE, WM, WN, 4, SIDE == 64 ? 2 : 1, SPLIT, STAGE, OUT><<<l.n_tiles, THREADS, 0, st>>>(o->mats, l.tiles, o->ws, o->sums, s, out);
+    k_ortho_product<SIDE, SIDE, WM, WN, 4, SIDE == 64 ? 2 : 1, SPLIT, STAGE, OUT><<<l.n_tiles, THREADS, 0, st>>>(l.tiles, o->ws, o->sums, s, out);
     if (l.n_cuts)
         k_ortho_join<SIDE, SPLIT, STAGE, OUT><<<l.n_cuts * (SIDE * SIDE / 8 / kThreads), kThreads, 0, st>>>(o->mats, l.cuts, o->ws, o->sums, s,
                                                                                                          out);
@@ -1218,7 +1217,7 @@ ds_status_t run(const ds_ortho *o, const void *src, const Out &out, hipStream_t 
     }
     auto grid = [](int64_t n) { return static_cast<unsigned>(n); };
     k_ortho_norm<SRC_BF16><<<grid(o->n_parts), kBlock, 0, st>>>(o->mats, o->parts, src, o->partial);
-    k_ortho_operands<SPLIT, SRC_BF16><<<grid(o->n_operands), kThreads, 0, st>>>(o->mats, o->operands, src, o->partial, o->cfg.eps, o->ws);
+    k_ortho_operands<SPLIT, SRC_BF16><<<grid(o->n_operands), kThreads, 0, st>>>(o->operands, src, o->partial, o->cfg.eps, o->ws);
     for (int32_t k = 0; k < o->cfg.steps; ++k) {
         const Step s{o->coef[3 * k], o->coef[3 * k + 1], o->coef[3 * k + 2], k & 1};
         product<SPLIT, kGram, 0>(o, s, out, st);
