@@ -215,6 +215,8 @@ __global__ __launch_bounds__(kBlock) void k_clip_update(const uint8_t *msg, floa
 template <int NB, class Tail>
 __global__ __launch_bounds__(kBlock) void k_clip_each(const uint8_t *msg, int64_t d, Tail tail)
 {
+    tail.ask();
+    ask_for(msg, d);
     const int64_t e = tail.first() + threadIdx.x * 4;
     if (e >= d) return;
     const uint32_t f = tail.wants(e, d);

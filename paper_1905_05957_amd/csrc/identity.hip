@@ -68,6 +68,8 @@ __global__ __launch_bounds__(kBlock) void k_identity_update(const float *q_in, f
 template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_identity_each(const float *q_in, int64_t d, Tail tail)
 {
+    tail.ask();
+    ask_for(q_in, d);
     const int64_t e = tail.first() + threadIdx.x * 4;
     if (e >= d) return;
     const uint32_t f = tail.wants(e, d);

@@ -335,6 +335,8 @@ template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_qsgd_each(const uint8_t *levels, const uint64_t *words, const float *norms, QParams P,
                                                       Tail tail)
 {
+    tail.ask();
+    ask_for(levels, words, norms, P.d, P.bshift, P.s);
     const int64_t e = tail.first() + threadIdx.x * 4;
     if (e >= P.d) return;
     const uint32_t f = tail.wants(e, P.d);

@@ -420,6 +420,8 @@ template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_rs_each(const uint64_t *__restrict__ words, const float *__restrict__ vals,
                                                     const uint32_t *__restrict__ off, int64_t d, int64_t n_sub, Tail tail)
 {
+    tail.ask();
+    ask_for(words, vals, off, d, n_sub);
     const int64_t e = tail.first() + threadIdx.x * 4;
     const int64_t sub = e >> 8;
     if (sub >= n_sub) return;                               // whole wavefronts

@@ -296,6 +296,8 @@ template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_sign_chunk_each(const uint64_t *__restrict__ words, const float *__restrict__ scales,
                                                             int64_t chunk, int64_t d, Tail tail)
 {
+    tail.ask();
+    ask_for(words, scales, chunk, d);
     const int64_t e = tail.first() + threadIdx.x * 4;
     if (e >= d) return;
     const uint32_t f = tail.wants(e, d);
@@ -1059,6 +1061,8 @@ template <class Tail>
 __global__ __launch_bounds__(kBlock) void k_sign_each(const uint64_t *__restrict__ words, const float *__restrict__ scales,
                                                       ds_sign_tables tb, int64_t d, Tail tail)
 {
+    tail.ask();
+    ask_for(words, scales, tb.tile_info, tb.piece_start, tb.piece_seg, tb.whole_d, d);
     const int64_t first = tail.first(), e = first + threadIdx.x * 4;
     if (e >= d) return;
     const uint32_t f = tail.wants(e, d);

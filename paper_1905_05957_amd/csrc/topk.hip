@@ -2183,6 +2183,8 @@ __global__ __launch_bounds__(kBlock) void k_topk_each(const u32x2 *pairs, int64_
 {
     __shared__ __attribute__((aligned(16))) float tilev[kTile];
     __shared__ int64_t range[2];
+    tail.ask();
+    ask_for(pairs, k, d);
     const int64_t base = tail.first();
     const int64_t e = base + threadIdx.x * 4;
     const uint32_t f = (e < d) ? tail.wants(e, d) : 0u;
