@@ -142,5 +142,4 @@ ds_status_t ds_identity_each(ds_ctx *c, const ds_payload_t *srv, const Tail &tai
     return ds_launch_status();
 }
 template ds_status_t ds_identity_each(ds_ctx *, const ds_payload_t *, const TailMomentum &, hipStream_t);
-template ds_status_t ds_identity_each(ds_ctx *, const ds_payload_t *, const TailAdamW<false> &, hipStream_t);
-template ds_status_t ds_identity_each(ds_ctx *, const ds_payload_t *, const TailAdamW<true> &, hipStream_t);
+template ds_status_t ds_identity_each(ds_ctx *, const ds_payload_t *, const TailAdamW &, hipStream_t);

@@ -37,14 +37,10 @@ __device__ __forceinline__ uint32_t quad_flags(int64_t e, int64_t d)
     return (e + 4 <= d) ? 15u : (1u << (d - e)) - 1u;
 }
 
-// Elements of p whose flag is set; the others read as 0 and are not touched.  STREAM: past the caches.
-template <bool STREAM>
+// Elements of p whose flag is set; the others read as 0 and are not touched.
 __device__ __forceinline__ f32x4 ld4_flags(const float *__restrict__ p, int64_t e, uint32_t f)
 {
-    if (f == 15u) {
-        const f32x4_any *at = reinterpret_cast<const f32x4_any *>(p + e);
-        return STREAM ? __builtin_nontemporal_load(at) : *at;
-    }
+    if (f == 15u) return __builtin_nontemporal_load(reinterpret_cast<const f32x4_any *>(p + e));
     f32x4 r = {0.f, 0.f, 0.f, 0.f};
     if (f & 1u) r.x = p[e];
     if (f & 2u) r.y = p[e + 1];
@@ -53,13 +49,10 @@ __device__ __forceinline__ f32x4 ld4_flags(const float *__restrict__ p, int64_t 
     return r;
 }
 
-template <bool STREAM>
 __device__ __forceinline__ void st4_flags(float *__restrict__ p, int64_t e, uint32_t f, f32x4 v)
 {
     if (f == 15u) {
-        f32x4_any *at = reinterpret_cast<f32x4_any *>(p + e);
-        if (STREAM) __builtin_nontemporal_store(static_cast<f32x4_any>(v), at);
-        else *at = v;
+        __builtin_nontemporal_store(static_cast<f32x4_any>(v), reinterpret_cast<f32x4_any *>(p + e));
         return;
     }
     if (f & 1u) p[e] = v.x;
@@ -84,11 +77,11 @@ struct TailMomentum : TailTiles {
     {
         f32x4 v = q;
         if (m) {
-            v = fma4(beta, ld4_flags<true>(m, e, f), q);
-            st4_flags<true>(m, e, f, v);
+            v = fma4(beta, ld4_flags(m, e, f), q);
+            st4_flags(m, e, f, v);
             if (u) v = fma4(beta, v, q);
         }
-        if (u) st4_flags<true>(u, e, f, v);
+        if (u) st4_flags(u, e, f, v);
     }
 };
 
@@ -96,9 +89,6 @@ struct TailMomentum : TailTiles {
 //   m <- fma(beta1, m, (1 - beta1) q) ; v <- fma(beta2, v, (1 - beta2) q q)
 //   x <- fma(-rate, m / (sqrt(v) * root + eps), keep * x)
 // with rate = gamma / (1 - beta1^(t+1)), root = 1 / sqrt(1 - beta2^(t+1)), keep = 1 - gamma * decay from the host, in 64 bits.
-// STREAM as ds_stream_worthwhile says: AdamW of 8, 12 and 16 M elements 31.5, 48.1 and 61.9 us with it, 29.0, 42.8 and 55.5
-// without; of 32 and 50 M 126 and 193 us with it, 135 and 219 without.
-template <bool STREAM>
 struct TailAdamW : TailTiles {
     const uint64_t *inside;
     float *x, *m, *v;
@@ -116,11 +106,11 @@ struct TailAdamW : TailTiles {
     }
     __device__ __forceinline__ void put(f32x4 q, int64_t e, int64_t, uint32_t f) const
     {
-        const f32x4 xv = ld4_flags<STREAM>(x, e, f), mo = ld4_flags<STREAM>(m, e, f), vo = ld4_flags<STREAM>(v, e, f);
+        const f32x4 xv = ld4_flags(x, e, f), mo = ld4_flags(m, e, f), vo = ld4_flags(v, e, f);
         const f32x4 mv = fma4(beta1, mo, rest1 * q), vv = fma4(beta2, vo, (rest2 * q) * q);
-        st4_flags<STREAM>(m, e, f, mv);
-        st4_flags<STREAM>(v, e, f, vv);
-        st4_flags<STREAM>(x, e, f, f32x4{step(xv.x, mv.x, vv.x), step(xv.y, mv.y, vv.y), step(xv.z, mv.z, vv.z), step(xv.w, mv.w, vv.w)});
+        st4_flags(m, e, f, mv);
+        st4_flags(v, e, f, vv);
+        st4_flags(x, e, f, f32x4{step(xv.x, mv.x, vv.x), step(xv.y, mv.y, vv.y), step(xv.z, mv.z, vv.z), step(xv.w, mv.w, vv.w)});
     }
 };
 
