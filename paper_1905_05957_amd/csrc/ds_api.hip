@@ -431,14 +431,16 @@ ds_status_t ds_apply_update_adamw(ds_ctx_t *c, const ds_ortho_t *skip, const ds_
     if (misaligned(x) || misaligned(m) || misaligned(v)) return DS_ERR_ALIGN;
     DeviceGuard guard(c->device);
     if (!guard.ok) return DS_ERR_DEVICE;
-    const double t = static_cast<double>(step) + 1.0;
     ds::TailTiles tiles{nullptr, static_cast<int32_t>(c->n_tiles)};
     if (skip) tiles.tiles = ds_ortho_tiles(skip, false, &tiles.n);
     if (tiles.n == 0) return DS_OK;                                         // the matrices are all of it
-    const ds::TailAdamW tail{tiles, skip ? ds_ortho_inside(skip) : nullptr, x, m, v, static_cast<float>(beta1),
-                             static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
-                             static_cast<float>(gamma / (1.0 - pow(beta1, t))), static_cast<float>(1.0 / sqrt(1.0 - pow(beta2, t))),
-                             static_cast<float>(eps), static_cast<float>(1.0 - gamma * decay)};
+    const uint64_t *inside = skip ? ds_ortho_inside(skip) : nullptr;
+    const double t = static_cast<double>(step) + 1.0;
+    const float b1 = static_cast<float>(beta1), rest1 = static_cast<float>(1.0 - beta1);
+    const float b2 = static_cast<float>(beta2), rest2 = static_cast<float>(1.0 - beta2);
+    const float rate = static_cast<float>(gamma / (1.0 - pow(beta1, t))), root = static_cast<float>(1.0 / sqrt(1.0 - pow(beta2, t)));
+    const float keep = static_cast<float>(1.0 - gamma * decay);
+    const ds::TailAdamW tail{tiles, inside, x, m, v, b1, rest1, b2, rest2, rate, root, static_cast<float>(eps), keep};
     return each(c, srv, tail, static_cast<hipStream_t>(hip_stream));
 }
 
