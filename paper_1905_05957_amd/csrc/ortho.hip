@@ -49,6 +49,7 @@ constexpr float kPolyScale = 4096.0f;          // B is held times 2^12 (entries 
 constexpr int kTileSide = 64;
 constexpr int kMaxParts = 512;                 // partial sums of a matrix's norm
 constexpr int64_t kPartElements = 16384;
+constexpr int64_t kMostBytes = 288000000000;   // of the workspace: the card's memory
 
 struct Mat {
     int64_t offset, ld;          // in the vector
@@ -62,7 +63,7 @@ struct Mat {
     float factor;
 };
 
-// What a workgroup of a product takes: tile (i, j) of a matrix, stages [k0, k1) of its sum.  slot < 0: the whole sum; else this
+// What a workgroup of a product takes: tile (i, j) of a matrix, panels [k0, k1) of its sum.  slot < 0: the whole sum; else this
 // part goes to that slot of the parts' buffer and a launch behind the product puts the parts together.
 // The matrix stands in it: a number of one would cost a second trip to memory before the first copy.
 struct Tile {
@@ -210,7 +211,8 @@ __global__ __launch_bounds__(kBlock) void k_ortho_norm(const Mat *__restrict__ m
 
 // X = U / (norm + eps), times 2^s, zero beyond the matrix.
 template <bool SPLIT, bool BF16>
-__global__ __launch_bounds__(kThreads) void k_ortho_operands(const Tile *__restrict__ tiles, const void *src, const double *__restrict__ partial, float eps, char *ws)
+__global__ __launch_bounds__(kThreads) void k_ortho_operands(const Tile *__restrict__ tiles, const void *src,
+                                                             const double *__restrict__ partial, float eps, char *ws)
 {
     constexpr int T = 64;
     __shared__ float tile[T][T + 1];
@@ -366,7 +368,8 @@ __device__ __forceinline__ void wait_copies()       // at most N copies of this 
 //
 // The wavefront multiplies Q' P': a lane then holds a row i of C and four consecutive j at a time.
 template <int TM, int TN, int WM, int WN, int S, int G, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
-__global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Tile *__restrict__ tiles, char *ws, float *parts, Step step, Out out)
+__global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Tile *__restrict__ tiles, char *ws,
+                                                                             float *parts, Step step, Out out)
 {
     constexpr int WAVES_N = TN / WN, WAVES = (TM / WM) * WAVES_N, FM = WM / 32, FN = WN / 32;
     constexpr bool ACROSS = STAGE >= kApply;                   // Q is X
@@ -1060,16 +1063,16 @@ double launch_time(const std::vector<Tile> &tiles, int side, bool split)
     return time;
 }
 
-// A product by tiles of `side`.  The device takes `at_once` workgroups; a workgroup's share of all stages is what it would have
+// A product by tiles of `side`.  The device takes `at_once` workgroups; a workgroup's share of all panels is what it would have
 // if they were dealt out evenly.  Tiles that fit into the shares stay whole; the others (those of a last round that would
 // leave most of the device idle, or sums longer than a share) are cut into parts that do, if `cutting`.
 void deal_out(const std::vector<Tile> &list, int side, bool cutting, Work &w)
 {
-    constexpr int kLeast = 8;              // stages of a part: below, filling the pipeline costs more than it saves
+    constexpr int kLeast = 8;              // panels of a part: below, filling the pipeline costs more than it saves
     const int at_once = tiles_at_once(side);
     w.side = side;
     std::vector<Tile> whole, cut, pieces;
-    int64_t total = 0, cut_stages = 0;
+    int64_t total = 0, cut_panels = 0;
     for (const Tile &t : list) total += t.k1;
     const int64_t share = std::max<int64_t>((total + at_once - 1) / at_once, kLeast);
     // the launch as the device would deal it out: every tile to the workgroup that is free first
@@ -1078,7 +1081,7 @@ void deal_out(const std::vector<Tile> &list, int side, bool cutting, Work &w)
     for (const Tile &t : list) {
         if (cutting && free_at.front() + t.k1 > share + share / 16 && t.k1 >= 2 * kLeast) {
             cut.push_back(t);
-            cut_stages += t.k1;
+            cut_panels += t.k1;
         } else {
             std::pop_heap(free_at.begin(), free_at.end(), later);
             free_at.back() += t.k1;
@@ -1086,7 +1089,7 @@ void deal_out(const std::vector<Tile> &list, int side, bool cutting, Work &w)
             whole.push_back(t);
         }
     }
-    const int64_t part = std::max<int64_t>(kLeast, (cut_stages + at_once - 1) / at_once);
+    const int64_t part = std::max<int64_t>(kLeast, (cut_panels + at_once - 1) / at_once);
     for (const Tile &t : cut) {
         const int32_t n = static_cast<int32_t>((t.k1 + part / 2) / part);
         if (n < 2) {
@@ -1096,7 +1099,7 @@ void deal_out(const std::vector<Tile> &list, int side, bool cutting, Work &w)
         w.cuts.push_back(Cut{t.mat, t.i, t.j, w.slots, n, {0, 0, 0}});
         for (int32_t p = 0; p < n; ++p) {
             Tile q = t;
-            q.k0 = static_cast<int32_t>(static_cast<int64_t>(t.k1 / 2) * p / n) * 2;           // even numbers of stages
+            q.k0 = static_cast<int32_t>(static_cast<int64_t>(t.k1 / 2) * p / n) * 2;           // even numbers of panels
             q.k1 = static_cast<int32_t>(static_cast<int64_t>(t.k1 / 2) * (p + 1) / n) * 2;
             q.slot = w.slots++;
             pieces.push_back(q);
@@ -1167,6 +1170,7 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
         return at;
     };
     for (int32_t k = 0; k < cfg.n_mats; ++k) {
+        if (t.ws_bytes > kMostBytes) return;         // will be refused; thin matrices can be 64 times what they hold
         Mat &M = t.mats[static_cast<size_t>(k)];
         const int64_t each = split ? 4 : 2;
         M.x[0] = take(static_cast<int64_t>(M.mp) * M.np * each);
@@ -1179,6 +1183,7 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
         t.n_partial += M.parts;
         for (int32_t p = 0; p < M.parts; ++p) t.parts.push_back(int2{k, p});
     }
+    if (t.ws_bytes > kMostBytes) return;
     plan_product(t.mats, kGram, split, t.gram);
     plan_product(t.mats, kPoly, split, t.poly);
     plan_product(t.mats, kApply, split, t.wide);
@@ -1325,6 +1330,10 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
         for (int32_t k = 0; k < 3 * cfg->steps; ++k) o->coef.push_back(cfg->coef ? cfg->coef[k] : standard[k % 3]);
         Tables t;
         make_tables(*cfg, o->split, t);
+        if (t.ws_bytes > kMostBytes) {
+            delete o;
+            return DS_ERR_DEVICE;
+        }
         o->n_operands = static_cast<int64_t>(t.operands.size());
         o->n_parts = static_cast<int64_t>(t.parts.size());
         int64_t bytes = 0;

@@ -99,3 +99,8 @@ def test_the_binding_checks_what_ctypes_would_cut():
         P.OrthoPlan(100, [(0, 2, 2)], scale="max")
     with pytest.raises(P.DsError):
         P.OrthoPlan(100, [])
+
+
+def test_more_workspace_than_the_card_has_is_refused_at_once():
+    # a row of 2^24 elements is worked on as 64 rows: 100 of them would take 860 GB, and tables of gigabytes
+    assert _create(d=2 ** 31 - 1, mats=[(k << 24, 0, 1, 1 << 24) for k in range(100)]) == DEVICE
