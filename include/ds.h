@@ -290,8 +290,11 @@ ds_status_t ds_server_aggregate_compress_update(ds_ctx_t *ctx, uint64_t step, co
  * Products: operands are held as the sum of two halves of 11 bits (three matrix products, sums in fp32), so results are
  * as those of fp32 products; with DS_ORTHO_HALF as one half of 11 bits (one product, a third of the arithmetic), for results
  * that are kept in bf16 or need no more.  They are scaled by powers of two, so small entries keep their bits.  Norms are
- * summed in fp64.  Range: singular values must stay below 2, which those of every list that converges for singular values
- * in [0, 1] do, and b t + c t^2 and a + b t + c t^2 within 15 for t in [0, 1] (else DS_ERR_CONFIG).  Sums are taken in a
+ * summed in fp64.  Range: the operands are held in half precision's range, so the singular values that a list of steps can make of
+ * those in [0, 1], its roundings included, must stay below 2.8 wherever a step starts from them, and b t + c t^2 and
+ * a + b t + c t^2 within 15 up to their squares t (else DS_ERR_CONFIG: those calls could end in NaN).  That a list converges
+ * does not suffice: 3, 0, 0 first leaves that range; and one that comes back from near 2 may fit with two halves and not with
+ * one.  Sums are taken in a
  * fixed order: equal calls on equal plans give equal bits.  What is not finite stays in its matrix.
  */
 typedef struct {

@@ -1245,16 +1245,46 @@ ds_status_t run(const ds_ortho *o, const void *src, const Out &out, hipStream_t 
     return o->split ? run<true, SRC_BF16, OUT>(o, src, out, st) : run<false, SRC_BF16, OUT>(o, src, out, st);
 }
 
-// B and, with two halves, B + a are held times kPolyScale: b t + c t^2 and a + b t + c t^2 must stay below 16 for the squared
-// singular values t, [0, 1] here; 15 leaves room for those that a step takes somewhat beyond 1.
-bool coefficients_fit(const float *q)
+// Whether every operand of a list of steps stays in the range in which it is held.  h bounds the singular values of the X that a
+// step reads: 1 at the start (the norm is Frobenius'), then the largest |p(s)|, p(s) = a s + b s^3 + c s^5, on [0, h] of the
+// step before.  Entries of a matrix do not exceed its largest singular value, so with t = s^2 those of G stay below h^2, which
+// times kGramScale has to be a half (65,504 at most: h <= 2.8), and those of B, a on its diagonal, below the largest
+// |a + b t + c t^2| on [0, h^2], times kPolyScale: 16; 15 leaves room for roundings, and holds for b t + c t^2 as well.
+// Rounding an operand moves its singular values by u of the largest one, 2^-11 with one half; with two, 2^-20 counts the sums in
+// fp32 too.  A list that comes back from near 2 lies on so steep a part of its polynomials that this decides: one half may
+// leave the range where two do not.
+bool coefficients_fit(const float *coef, int32_t steps, bool split)
 {
-    const double a = q[0], b = q[1], c = q[2];
-    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-    double ends[3] = {0.0, 1.0, 0.0};
-    if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < 1.0) ends[2] = -b / (2.0 * c);
-    for (double t : ends)
-        if (std::fabs(b * t + c * t * t) > 15.0 || std::fabs(a + b * t + c * t * t) > 15.0) return false;
+    const double u = split ? 0x1p-20 : 0x1p-11;
+    double h = 1.0;
+    for (int32_t k = 0; k < steps; ++k) {
+        const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
+        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        h *= 1.0 + u;
+        if (!(h <= 2.8)) return false;
+        const double top = h * h;
+        // extremes of b t + c t^2 and of p: at the ends and where the derivatives b + 2 c t and a + 3 b t + 5 c t^2 vanish
+        double at[5] = {0.0, top, 0.0, 0.0, 0.0};
+        if (c != 0.0) at[2] = -b / (2.0 * c);
+        const double q = 9.0 * b * b - 20.0 * a * c;
+        if (c == 0.0 && b != 0.0) at[3] = -a / (3.0 * b);
+        if (c != 0.0 && q >= 0.0) {
+            // the root without cancellation, and the other from their product a / (5 c)
+            const double r = -0.5 * (3.0 * b + std::copysign(std::sqrt(q), b));
+            at[3] = r / (5.0 * c);
+            if (r != 0.0) at[4] = a / r;
+        }
+        double poly = 0.0, next = 0.0;
+        for (double t : at) {
+            if (!(t >= 0.0 && t <= top)) continue;
+            const double v = b * t + c * t * t;
+            if (std::fabs(v) > 15.0 || std::fabs(a + v) > 15.0) return false;
+            poly = std::max(poly, std::fabs(a + v));
+            next = std::max(next, std::sqrt(t) * std::fabs(a + v));
+        }
+        // G off by u h^2 moves B by the steepest b + 2 c t times that
+        h = next + h * u * (top * std::max(std::fabs(b), std::fabs(b + 2.0 * c * top)) + poly);
+    }
     return true;
 }
 
@@ -1289,9 +1319,7 @@ ds_status_t ds_ortho_create(const ds_ortho_config_t *cfg, ds_ortho_t **out)
     if (!(cfg->eps >= 0.f) || !std::isfinite(cfg->eps)) return DS_ERR_CONFIG;
     if (cfg->factor < DS_ORTHO_FACTOR_NONE || cfg->factor > DS_ORTHO_FACTOR_RMS) return DS_ERR_CONFIG;
     if (cfg->flags & ~(DS_ORTHO_NESTEROV | DS_ORTHO_HALF)) return DS_ERR_CONFIG;
-    if (cfg->coef)
-        for (int32_t k = 0; k < cfg->steps; ++k)
-            if (!coefficients_fit(cfg->coef + 3 * k)) return DS_ERR_CONFIG;
+    if (cfg->coef && !coefficients_fit(cfg->coef, cfg->steps, !(cfg->flags & DS_ORTHO_HALF))) return DS_ERR_CONFIG;
     for (int32_t k = 0; k < cfg->n_mats; ++k) {
         const ds_matrix_t &M = cfg->mats[k];
         if (M.rows < 1 || M.cols < 1 || M.offset < 0 || std::min(M.rows, M.cols) > 32768 || std::max(M.rows, M.cols) > (1 << 24)) return DS_ERR_SHAPE;
