@@ -287,10 +287,12 @@ ds_status_t ds_server_aggregate_compress_update(ds_ctx_t *ctx, uint64_t step, co
  * offset and row stride (column blocks of one wider array are matrices with its row length as their ld) but no
  * element may belong to two of them.  Elements in no matrix are not read and not written.
  *
- * Products: operands are held as the sum of two halves of 11 bits (three matrix products, sums in fp32), so results are
- * as those of fp32 products; with DS_ORTHO_HALF as one half of 11 bits (one product, a third of the arithmetic), for results
- * that are kept in bf16 or need no more.  They are scaled by powers of two, so small entries keep their bits.  Norms are
- * summed in fp64.  Range: the operands are held in half precision's range, so the singular values that a list of steps can make of
+ * Products: operands are held as the sum of two halves of 11 bits (three matrix products, sums in fp32), so results err
+ * as those of fp32 products do; with DS_ORTHO_HALF as one half of 11 bits (one product, a third of the arithmetic), for results
+ * that are kept in bf16 or need no more.  They are scaled by powers of two: an entry of U / ||U|| is off by
+ * 2^-22 of itself or by 2^-39, whichever is more, an entry of G by 2^-38, of B by 2^-37.  So the results' errors are small
+ * against the whole matrix; rows or columns whose entries lie below 2^-17 of the norm have fewer bits, which shows where many
+ * steps draw them up to the others (rows of 1e-6 of the others: off by 4e-4 of themselves).  Norms are summed in fp64.  Range: the operands are held in half precision's range, so the singular values that a list of steps can make of
  * those in [0, 1], its roundings included, must stay below 2.8 wherever a step starts from them, and b t + c t^2 and
  * a + b t + c t^2 within 15 up to their squares t (else DS_ERR_CONFIG: those calls could end in NaN).  That a list converges
  * does not suffice: 3, 0, 0 first leaves that range; and one that comes back from near 2 may fit with two halves and not with

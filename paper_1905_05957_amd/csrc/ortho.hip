@@ -9,8 +9,11 @@
 // Operands.  An fp32 value is held as hi + lo, two IEEE halves of 11 bits, hi = RN16(x), lo = RN16(x - hi), and a product of
 // such operands is hi hi + hi lo + lo hi on the matrix cores with one fp32 sum: 22 bits, what is left out is 2^-22 of the
 // product.  Half precision rather than bf16 because entries are bounded (|X| <= 1, singular values at most about 1.2): three
-// more bits of significand per product for the same rate; the range is used by scaling with powers of two: X by 2^s with
-// entries near 16 for an orthogonal matrix, G by 2^13 and B by 2^12, which leaves entries of lo 2^-20 below those of X.
+// more bits of significand per product for the same rate; the range is used by scaling with powers of two, X by 2^14, G by 2^13 and
+// B by 2^12, the largest that their bounds allow.  Where lo falls below the smallest half, 2^-24, bits are lost: an entry of X is
+// off by 2^-22 of itself or by 2^-39 of the norm, whichever is more, so rows and columns with entries below 2^-17 of the norm
+// keep fewer than 22 bits.  (300 x 700, every other row times 1e-6: those rows are off by 3.6e-4 of themselves; by 1.1e-2 if X is
+// scaled for entries near 16 in an orthogonal matrix, 2^9 here.)
 // With one half (DS_ORTHO_HALF) a rounding is 2^-11 at most; it grows with the smallest singular values at most, 3.44^5 = 485 times
 // while an entry of X grows as much or reaches 1 / sqrt(n), so it ends below a rounding to bf16.
 //
@@ -44,6 +47,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
 constexpr int kRow = 64;                       // bytes of a row in a panel
+constexpr float kOperandScale = 16384.0f;      // X is held times 2^14 (entries up to 4)
 constexpr float kGramScale = 8192.0f;          // G is held times 2^13 (entries up to 8)
 constexpr float kPolyScale = 4096.0f;          // B is held times 2^12 (entries up to 16)
 constexpr int kTileSide = 64;
@@ -209,7 +213,7 @@ __global__ __launch_bounds__(kBlock) void k_ortho_norm(const Mat *__restrict__ m
     if (threadIdx.x == 0) partial[M.part0 + pt.y] = s;
 }
 
-// X = U / (norm + eps), times 2^s, zero beyond the matrix.
+// X = U / (norm + eps), times M.scale, zero beyond the matrix.
 template <bool SPLIT, bool BF16>
 __global__ __launch_bounds__(kThreads) void k_ortho_operands(const Tile *__restrict__ tiles, const void *src,
                                                              const double *__restrict__ partial, float eps, char *ws)
@@ -1148,11 +1152,7 @@ void make_tables(const ds_ortho_config_t &cfg, bool split, Tables &t)
         M.mp = static_cast<int32_t>(round_up(M.m, kTileSide));
         M.np = static_cast<int32_t>(round_up(M.n, kTileSide));
         M.panel = M.mp * kRow;
-        // entries of an orthogonal [m, n] matrix are about 1 / sqrt(n); 16 there leaves 2^-25 of an entry to lo, and
-        // 2^14 keeps the largest possible one, singular value 2, below the largest half (65,504)
-        int s = 4;
-        while (s < 14 && (1ll << (2 * (s - 4))) < M.n) ++s;
-        M.scale = static_cast<float>(1 << s);
+        M.scale = kOperandScale;
         const double aspect = static_cast<double>(in.rows) / in.cols;
         M.factor = cfg.factor == DS_ORTHO_FACTOR_ASPECT ? static_cast<float>(sqrt(std::max(1.0, aspect)))
                    : cfg.factor == DS_ORTHO_FACTOR_RMS ? static_cast<float>(0.2 * sqrt(static_cast<double>(M.n))) : 1.0f;
