@@ -288,16 +288,20 @@ ds_status_t ds_server_aggregate_compress_update(ds_ctx_t *ctx, uint64_t step, co
  * element may belong to two of them.  Elements in no matrix are not read and not written.
  *
  * Products: operands are held as the sum of two halves of 11 bits (three matrix products, sums in fp32), so results err
- * as those of fp32 products do; with DS_ORTHO_HALF as one half of 11 bits (one product, a third of the arithmetic), for results
- * that are kept in bf16 or need no more.  They are scaled by powers of two: an entry of U / ||U|| is off by
- * 2^-22 of itself or by 2^-39, whichever is more, an entry of G by 2^-38, of B by 2^-37.  So the results' errors are small
- * against the whole matrix; rows or columns whose entries lie below 2^-17 of the norm have fewer bits, which shows where many
- * steps draw them up to the others (rows of 1e-6 of the others: off by 4e-4 of themselves).  Norms are summed in fp64.  Range: the operands are held in half precision's range, so the singular values that a list of steps can make of
- * those in [0, 1], its roundings included, must stay below 2.8 wherever a step starts from them, and b t + c t^2 and
- * a + b t + c t^2 within 15 up to their squares t (else DS_ERR_CONFIG: those calls could end in NaN).  That a list converges
- * does not suffice: 3, 0, 0 first leaves that range; and one that comes back from near 2 may fit with two halves and not with
- * one.  Sums are taken in a
- * fixed order: equal calls on equal plans give equal bits.  What is not finite stays in its matrix.
+ * as those of fp32 products do: 1e-6 (noise) to 1.6e-4 (rank 1) of the whole matrix after the standard five steps, 0.6
+ * to 1.4 times what fp32 products give.  With DS_ORTHO_HALF they are one half of 11
+ * bits: one product, a third of the arithmetic.  Its roundings grow in all weak directions by the product of the steps' a (485 times
+ * in the standard five), so results are off by 1e-3 for noise, 4e-3 for singular values 1 / k, 1.2e-2 for 1 / k^1.5, 4e-2 for rank
+ * 16 and 0.15 for rank 1, whatever type they are kept in (a rounding to bf16: 1.7e-3).
+ * Operands are scaled by powers of two: an entry of U / ||U|| is off by 2^-22 of itself (one half: 2^-11) or by 2^-39, whichever
+ * is more, an entry of G by 2^-38, of B by 2^-37.  So errors are small against the whole matrix; rows or columns whose
+ * entries lie below 2^-17 of the norm have fewer bits, which shows where many steps draw them up to the others (rows of 1e-6
+ * of the others: off by 4e-4 of themselves).  Norms are summed in fp64.
+ * Range: the operands are held in half precision's range, so the singular values that a list of steps can make of those in [0, 1],
+ * its roundings included, must stay below 2.8 wherever a step starts from them, and b t + c t^2 and a + b t + c t^2 within
+ * 15 up to their squares t (else DS_ERR_CONFIG: those calls could end in NaN).  That a list converges does not suffice: 3, 0, 0
+ * first leaves that range; and one that comes back from near 2 may fit with two halves and not with one.
+ * Sums are taken in a fixed order: equal calls on equal plans give equal bits.  What is not finite stays in its matrix.
  */
 typedef struct {
     int64_t offset;           /* of element (0, 0) in the vector */

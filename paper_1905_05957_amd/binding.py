@@ -454,7 +454,9 @@ class OrthoPlan:
     current device.
 
     mats: (offset, rows, cols) or (offset, rows, cols, row stride) of each matrix; coef: (a, b, c) for every step, or a list
-    of one such triple per step; scale: "none", "aspect" or "rms", the factor of an orthogonalised matrix; half: products of half precision, a third of the time.
+    of one such triple per step; scale: "none", "aspect" or "rms", the factor of an orthogonalised matrix; half: products of half
+    precision, a third of the arithmetic and about half the time, off by 1e-3 of the whole for noise and by up to 0.15 where
+    a matrix has only a few strong directions (include/ds.h).
     """
 
     def __init__(self, d: int, mats, steps: int = 5, coef=None, eps: float = 1e-7, scale="none", nesterov: bool = False,

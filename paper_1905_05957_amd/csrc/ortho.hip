@@ -14,8 +14,16 @@
 // off by 2^-22 of itself or by 2^-39 of the norm, whichever is more, so rows and columns with entries below 2^-17 of the norm
 // keep fewer than 22 bits.  (300 x 700, every other row times 1e-6: those rows are off by 3.6e-4 of themselves; by 1.1e-2 if X is
 // scaled for entries near 16 in an orthogonal matrix, 2^9 here.)
-// With one half (DS_ORTHO_HALF) a rounding is 2^-11 at most; it grows with the smallest singular values at most, 3.44^5 = 485 times
-// while an entry of X grows as much or reaches 1 / sqrt(n), so it ends below a rounding to bf16.
+// Roundings of X lie in all directions, and those of singular values near zero grow by a in every step, 3.44^5 = 485 times, while
+// the strong ones stay near 1.  Where all are of one size the entries of X grow with the roundings; where a few
+// fill the entries they do not.  768 x 2048, off by (relative to the whole, in fp32; rounding to bf16: 1.7e-3)
+//                                    two halves   fp32 products   one half (DS_ORTHO_HALF)
+//   noise                               2.3e-6        3.6e-6        1.1e-3
+//   singular values 1 / k               4.6e-6        4.2e-6        4.0e-3
+//   1 / k^1.5                           1.3e-5        1.6e-5        1.2e-2
+//   rank 16                             5.7e-5        4.3e-5        4.6e-2
+//   rank 2                              7.4e-5        8.5e-5        7.1e-2
+//   rank 1                              1.4e-4        2.3e-4        1.5e-1
 //
 // Layout.  An operand lies in panels of 16 columns (32 with one half): row after row 64 bytes, 16 hi and 16 lo (32 halves).  A
 // stage of a product, 16 (32) values of k, is then one contiguous piece of a tile's rows when k runs along the rows, and
@@ -322,9 +330,11 @@ __device__ __forceinline__ float old_scale(const Step &step)
     return STAGE == kPoly ? step.b * (kPolyScale / kGramScale) : 0.f;
 }
 
-// a lies on B's diagonal, rounded as B is, so the last product does not read X a second time.  With one half that rounding is
-// 2^-11 of a row at most, as X's own is; results in bf16 lie 1.9e-3 (root mean square, relative) from those in 64 bits with
-// it and 2.0e-3 with a applied to X in fp32; rounding to bf16 alone is 1.66e-3.
+// a lies on B's diagonal, rounded as B is, so the last product does not read X a second time (124 M elements in fp32 3.79 ms, 3.94
+// with a applied to X).  Its rounding is 2^-22 or 2^-11 of a row at most, as X's own is; but the sums hold a x from that
+// panel on, and each of their roundings is relative to it: with two halves a rank of 16 comes out twice as far off as with a applied to X
+// in fp32 (by an emulation), 1.3 times as far as by fp32 products (measured), matrices without strong directions nearer
+// than those.  With one half results in bf16 of noise lie 1.9e-3 from those in 64 bits with it and 2.0e-3 without.
 template <int STAGE>
 constexpr bool kReadsOld = STAGE == kPoly;
 
