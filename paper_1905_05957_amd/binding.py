@@ -169,6 +169,14 @@ def _stream_ptr(stream, device=None) -> Optional[int]:
     return C.c_void_p(stream.cuda_stream)
 
 
+def _signed(value, bits: int, what: str) -> int:
+    """`value` as a number that the C structure holds; ctypes would cut it."""
+    value = int(value)
+    if not -(1 << (bits - 1)) <= value < 1 << (bits - 1):
+        raise ValueError(f"{what}: {value} is no {bits}-bit number")
+    return value
+
+
 def _one_device(device, **tensors) -> None:
     for what, t in tensors.items():
         if t is not None and t.device != device:
@@ -462,26 +470,26 @@ class OrthoPlan:
     def __init__(self, d: int, mats, steps: int = 5, coef=None, eps: float = 1e-7, scale="none", nesterov: bool = False,
                  half: bool = False):
         L = load_library()
-        rows = [tuple(int(v) for v in m) for m in mats]
+        rows = [tuple(m) for m in mats]
         if any(len(m) not in (3, 4) for m in rows):
             raise ValueError("mats: (offset, rows, cols) or (offset, rows, cols, row stride) of each matrix")
-        if any(not -2 ** 31 <= v < 2 ** 31 for m in rows for v in m[1:3]):
-            raise ValueError("mats: rows and columns are 32-bit numbers")
+        rows = [tuple(_signed(v, bits, "mats") for v, bits in zip(m, (64, 32, 32, 64))) for m in rows]
+        d, steps = _signed(d, 64, "d"), _signed(steps, 32, "steps")
         arr = (ds_matrix_t * max(1, len(rows)))(*[ds_matrix_t(m[0], m[3] if len(m) == 4 else m[2], m[1], m[2]) for m in rows])
         cfg = ds_ortho_config_t()
-        cfg.d, cfg.mats, cfg.n_mats, cfg.steps = int(d), arr, len(rows), int(steps)
-        cfg.eps, cfg.factor = float(eps), _FACTOR[scale] if isinstance(scale, str) else int(scale)
+        cfg.d, cfg.mats, cfg.n_mats, cfg.steps = d, arr, len(rows), steps
+        cfg.eps, cfg.factor = float(eps), _FACTOR[scale] if isinstance(scale, str) else _signed(scale, 32, "scale")
         cfg.flags = (ORTHO_NESTEROV if nesterov else 0) | (ORTHO_HALF if half else 0)
         if coef is not None:
             c = np.asarray(coef, dtype=np.float32)
             if c.shape == (3,):
-                c = np.tile(c, (max(1, int(steps)), 1))
-            if c.shape != (int(steps), 3):
-                raise ValueError(f"coef: shape {c.shape}, expected (3,) or ({int(steps)}, 3)")
+                c = np.tile(c, (min(max(1, steps), 32), 1))          # more steps are refused before the list is read
+            elif c.shape != (steps, 3):
+                raise ValueError(f"coef: shape {c.shape}, expected (3,) or ({steps}, 3)")
             c = np.ascontiguousarray(c)
             cfg.coef = c.ctypes.data_as(C.POINTER(C.c_float))
         self._h = C.c_void_p()
-        self.d, self.steps = int(d), int(steps)
+        self.d, self.steps = d, steps
         _check(L.ds_ortho_create(C.byref(cfg), C.byref(self._h)), "ds_ortho_create")
         self.device = torch.device("cuda", torch.cuda.current_device())
 
