@@ -274,6 +274,13 @@ __global__ __launch_bounds__(kThreads) void k_ortho_operands(const Tile *__restr
 // ---------------------------------------------------------------------------------------
 enum Stage { kGram, kPoly, kApply, kLast };    // G = X X' ; B = b G + c G G ; X <- a X + B X ; the same into the vector
 
+constexpr int kStages = 4;                     // of a product's copies in LDS
+
+// Whether sums may be cut into parts.  Tiles of 64 x 64 are for few or small ones, and then only G's sums, as long as the longer
+// side, are worth a second launch: of 15,000 plans of 1 to 120 matrices up to 3000 x 3000, 769 cut G on such tiles and none B or X.
+template <int SIDE, int STAGE>
+constexpr bool kCanCut = SIDE != kTileSide || STAGE == kGram;
+
 struct Step {
     float a, b, c;
     int from;                  // which of the two X the step starts from
@@ -291,7 +298,8 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // Direct copy of 16 bytes per lane, from `base` + `offset` into LDS at `lds` + 16 l for lane l; `base` and `lds` are the same for
 // the wavefront.  It has no output register.  Written as an instruction because the compiler waits for every
 // outstanding copy of its own builtin before the next read of LDS, also of another stage; the wait that is needed
-// stands in front of the barrier of that stage.  m0 is a register the compiler does not allocate; nothing else here uses it.
+// stands in front of the barrier of that stage.  m0 is reserved (named as clobbered the compiler warns of it): nothing is allocated to
+// it, the compiler sets it right before an instruction of its own that reads it, and in these kernels there is none.
 __device__ __forceinline__ void copy_to_lds(const char *base, uint32_t offset, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory");
@@ -372,7 +380,7 @@ __device__ __forceinline__ void wait_copies()       // at most N copies of this 
 // of k as well; Q = X, in the last product, lies with k across the rows: its tile is transposed on the way from LDS to the
 // registers.
 //
-// Pipeline.  LDS holds S stages of G panels, of 16 (32) values of k each.  While a panel is multiplied from registers, the
+// Pipeline.  LDS holds kStages stages of G panels, of 16 (32) values of k each.  While a panel is multiplied from registers, the
 // fragments of the next are read from LDS and the copies of the stages behind, which pass no registers, are under way; one
 // barrier a stage.  (Small tiles, whose panels are a few instructions, take two panels a stage.)
 //
@@ -381,16 +389,16 @@ __device__ __forceinline__ void wait_copies()       // at most N copies of this 
 // different banks: 267 and 228 bytes a clock measured, 43 and 80 without.
 //
 // The wavefront multiplies Q' P': a lane then holds a row i of C and four consecutive j at a time.
-template <int TM, int TN, int WM, int WN, int S, int G, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
+template <int TM, int TN, int WM, int WN, int G, bool SPLIT, int STAGE, int OUT>      // OUT: 0 fp32, 1 bf16, 2 the model
 __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(const Tile *__restrict__ tiles, char *ws,
                                                                              float *parts, Step step, Out out)
 {
-    constexpr int WAVES_N = TN / WN, WAVES = (TM / WM) * WAVES_N, FM = WM / 32, FN = WN / 32;
+    constexpr int S = kStages, WAVES_N = TN / WN, WAVES = (TM / WM) * WAVES_N, FM = WM / 32, FN = WN / 32;
     constexpr bool ACROSS = STAGE >= kApply;                   // Q is X
     constexpr int K = kPanel<SPLIT>, PIECE = K * kRow;         // values of k in a stage; a panel's part of a stage of X
     constexpr int PBYTES = TM * kRow, QBYTES = TN * kRow, PANEL_BYTES = PBYTES + QBYTES, STAGE_BYTES = G * PANEL_BYTES;
     constexpr int PCOPIES = PBYTES / (WAVES * 1024), QCOPIES = QBYTES / (WAVES * 1024), COPIES = G * (PCOPIES + QCOPIES);
-    static_assert(PCOPIES * WAVES * 1024 == PBYTES && QCOPIES * WAVES * 1024 == QBYTES && (S == 3 || S == 4) && (G == 1 || G == 2), "tile");
+    static_assert(PCOPIES * WAVES * 1024 == PBYTES && QCOPIES * WAVES * 1024 == QBYTES && (G == 1 || G == 2), "tile");
     __shared__ __attribute__((aligned(256))) char lds[S * STAGE_BYTES];
     const Tile &tl = tiles[blockIdx.x];
     const Mat &M = tl.m;
@@ -524,7 +532,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     auto cross = [&](auto steady, int k, const Frags &now, Frags &next) {
         const int under_way = stages - 2 - k;              // stages after the next that have been asked for
         if (decltype(steady)::value || under_way >= S - 2) wait_copies<(S - 2) * COPIES>();
-        else if (S > 3 && under_way == S - 3) wait_copies<(S - 3) * COPIES>();
+        else if (under_way == S - 3) wait_copies<(S - 3) * COPIES>();
         else wait_copies<0>();
         // everybody's copies of stage k + 1 are there, and everybody holds the end of stage k in registers
         __builtin_amdgcn_s_barrier();
@@ -557,7 +565,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / WN) * 64) void k_ortho_product(co
     }
     multiply(f1);
 
-    if (tl.slot >= 0) {
+    if (kCanCut<TM, STAGE> && tl.slot >= 0) {
         // eight columns of all rows behind each other: what 64 threads of the joining launch read lies together
         float *mine = parts + static_cast<int64_t>(tl.slot) * (TM * TN);
 #pragma unroll
@@ -1131,6 +1139,7 @@ void plan_product(const std::vector<Mat> &mats, int stage, bool split, Work &bes
     for (int side : {64, 128, 256}) {
         const std::vector<Tile> list = list_tiles(mats, side, stage, split ? kPanel<true> : kPanel<false>);
         for (bool cutting : {false, true}) {
+            if (cutting && side == kTileSide && stage != kGram) continue;      // kCanCut
             Work w;
             deal_out(list, side, cutting, w);
             if (cutting && w.cuts.empty()) continue;
@@ -1204,10 +1213,12 @@ template <int SIDE, bool SPLIT, int STAGE, int OUT>
 void product_of(const ds_ortho *o, const ds_ortho::Launch &l, const Step &s, const Out &out, hipStream_t st)
 {
     constexpr int WM = SIDE == 64 ? 32 : SIDE == 128 ? 64 : 128, WN = SIDE == 64 ? 32 : 64, THREADS = (SIDE / WM) * (SIDE / WN) * 64;
-    k_ortho_product<SIDE, SIDE, WM, WN, 4, SIDE == 64 ? 2 : 1, SPLIT, STAGE, OUT><<<l.n_tiles, THREADS, 0, st>>>(l.tiles, o->ws, o->sums, s, out);
-    if (l.n_cuts)
-        k_ortho_join<SIDE, SPLIT, STAGE, OUT><<<l.n_cuts * (SIDE * SIDE / 8 / kThreads), kThreads, 0, st>>>(o->mats, l.cuts, o->ws, o->sums, s,
-                                                                                                         out);
+    k_ortho_product<SIDE, SIDE, WM, WN, SIDE == 64 ? 2 : 1, SPLIT, STAGE, OUT><<<l.n_tiles, THREADS, 0, st>>>(l.tiles, o->ws, o->sums, s, out);
+    if constexpr (kCanCut<SIDE, STAGE>) {
+        if (l.n_cuts)
+            k_ortho_join<SIDE, SPLIT, STAGE, OUT><<<l.n_cuts * (SIDE * SIDE / 8 / kThreads), kThreads, 0, st>>>(o->mats, l.cuts, o->ws, o->sums,
+                                                                                                             s, out);
+    }
 }
 
 template <bool SPLIT, int STAGE, int OUT>
