@@ -333,9 +333,10 @@ typedef struct {
 
 typedef struct ds_ortho ds_ortho_t;
 
-/* Creates a plan on the current device with its tables and its workspace (4 bytes per element of the vector and about 12 per
- * element of the matrices, half of that with DS_ORTHO_HALF, each matrix's sides rounded up to multiples of 64; none of the
- * latter where all matrices are small, up to 64 x 512 or 128 x 128).  Errors: NULL, SHAPE (d, n_mats, steps or a matrix out
+/* Creates a plan on the current device with its tables and its workspace: 4.2 bytes per element of the vector; and, unless
+ * all matrices are small (up to 64 x 512 or 128 x 128), 8 m (m + n) bytes for each, m <= n its sides rounded up to multiples
+ * of 64 (8 per element of a long one to 16 of a square one; half of that with DS_ORTHO_HALF), 0.3 m n for tables, and
+ * where sums are cut into parts up to 100 MB for those.  Errors: NULL, SHAPE (d, n_mats, steps or a matrix out
  * of range), CONFIG (bad enum or flag, eps negative or not finite, coefficients out of range, two matrices that share an
  * element), DEVICE (memory).
  * Calls with one plan share its workspace: they must not overlap (one stream, or ordered by events; that holds for

@@ -71,3 +71,16 @@ def test_together_they_launch_every_kernel_of_tiles():
                     assert ("product", side, two, product, kind) in reached
                     if side > 64 or product == G:
                         assert ("join", side, two, product, kind) in reached
+
+
+def test_the_memory_is_what_the_header_says(launches):
+    up = lambda v: (v + 63) // 64 * 64                    # noqa: E731
+    for (half, mats, tiles), (got, _) in zip(PLANS, launches([(half, mats, 0) for half, mats, _ in PLANS])):
+        d = sum(r * c for r, c in mats)
+        sides = [(up(min(m)), up(max(m))) for m in mats]
+        least = 4 * d + sum((4 if half else 8) * m * (m + n) for m, n in sides)
+        most = 4.2 * d + sum((4 if half else 8) * m * (m + n) + 0.3 * m * n for m, n in sides) + (1e8 if "c" in tiles else 0) + 65536
+        assert least <= got <= most, (mats[0], got, least, most)
+    small = [(64, 512)] * 100 + [(100, 128)] * 50
+    (got, _), = launches([(False, small, 0)])
+    assert got <= 4.2 * sum(r * c for r, c in small) + 65536
