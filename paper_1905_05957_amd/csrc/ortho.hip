@@ -61,7 +61,9 @@ constexpr float kPolyScale = 4096.0f;          // B is held times 2^12 (entries 
 constexpr int kTileSide = 64;
 constexpr int kMaxParts = 512;                 // partial sums of a matrix's norm
 constexpr int64_t kPartElements = 16384;
-constexpr int64_t kMostBytes = 288000000000;   // of the workspace: the card's memory
+// A workspace beyond this, all of the card's memory, is refused before its tables are made, which would be gigabytes; one that
+// is more than what is free is refused by its allocation.
+constexpr int64_t kMostBytes = 288000000000;
 
 struct Mat {
     int64_t offset, ld;          // in the vector
@@ -1087,7 +1089,8 @@ double launch_time(const std::vector<Tile> &tiles, int side, bool split)
 
 // A product by tiles of `side`.  The device takes `at_once` workgroups; a workgroup's share of all panels is what it would have
 // if they were dealt out evenly.  Tiles that fit into the shares stay whole; the others (those of a last round that would
-// leave most of the device idle, or sums longer than a share) are cut into parts that do, if `cutting`.
+// leave most of the device idle, or sums longer than a share) are cut into parts that do, if `cutting`.  The parts are for all that
+// the device takes at once, two workgroups per compute unit below 256 x 256; parts for one per unit were not tried.
 void deal_out(const std::vector<Tile> &list, int side, bool cutting, Work &w)
 {
     constexpr int kLeast = 8;              // panels of a part: below, filling the pipeline costs more than it saves

@@ -2,7 +2,8 @@
 // consecutive elements e..e+3 of its row (e a multiple of 4, e < d),
 //   wants(e, d)      the flags of the elements that take part; none: the pass may leave at once
 //   put(q, e, d, f)  the decoded elements and those flags
-// after ask() at its top, and takes the 2048-element tile that `tiles` lists for its workgroup: those with an element that takes part (nullptr: all).
+// after ask() at its top, and takes the 2048-element tile that `tiles` lists for its workgroup: those with an element that
+// takes part (nullptr: all).
 // Matrices of a plan are marked in a plane of bits (bit j & 63 of word j >> 6) that covers ceil(d / 64) words: a quad costs one
 // byte of it, and the matrices may lie anywhere, column blocks of a wider array among them.
 #pragma once
@@ -88,10 +89,10 @@ struct TailMomentum : TailTiles {
 // AdamW on every element outside the matrices (inside == nullptr: on all of them):
 //   m <- fma(beta1, m, (1 - beta1) q) ; v <- fma(beta2, v, (1 - beta2) q q)
 //   x <- fma(-rate, m / (sqrt(v) * root + eps), keep * x)
+// with rate = gamma / (1 - beta1^(t+1)), root = 1 / sqrt(1 - beta2^(t+1)), keep = 1 - gamma * decay from the host, in 64 bits.
 // Bound by memory: 24 bytes an element and the message, 124 M elements in 0.515 ms, 5.8 TB/s.  Past the caches at every size: a
 // training step in between leaves nothing of x, m and v in them (11.2 M elements 56 us on buffers that were not touched
 // since, 61 us with ordinary accesses; called again on the same buffers 57 and 48).
-// with rate = gamma / (1 - beta1^(t+1)), root = 1 / sqrt(1 - beta2^(t+1)), keep = 1 - gamma * decay from the host, in 64 bits.
 struct TailAdamW : TailTiles {
     const uint64_t *inside;
     float *x, *m, *v;
