@@ -29,7 +29,7 @@
 // stage of a product, 16 (32) values of k, is then one contiguous piece of a tile's rows when k runs along the rows, and
 // pieces of 1 KB (2 KB) when k runs across them.
 //
-// What bounds it.  One 4096 x 4096: the matrix cores and the power they draw: B X of 256 x 256 tiles runs at 1.2 to 1.33 PFLOP/s of
+// What bounds it.  One 4096 x 4096: the matrix cores and the power they draw: B X of 256 x 256 tiles runs at 1.1 to 1.3 PFLOP/s of
 // half-precision products with the cores busy 75 % of the cycles at 1.65 GHz (the libraries' product of that size: 1.36).  G and
 // B, 0.52 of the arithmetic each by symmetry, 1.1.  Many matrices of width 768: every tile is 48 (24) panels, and its first
 // copies and results, 13 (7) us, come at the same time on all compute units: 0.9 (0.65) PFLOP/s.  Sums shorter still, or few
@@ -745,7 +745,9 @@ template <bool SPLIT>
 int64_t small_bytes(int64_t mp, int64_t np) { return (mp * np + mp * mp) * (SPLIT ? 4 : 2); }
 
 // Norm, operands, all steps and the result of one matrix, X [MP, np] and G (B in its place) in LDS.  Chains of small
-// dependent products are bound by latency: five steps on 96 x 64 took 17 launches and 54 us, 25 us so.
+// dependent products are bound by latency: five steps on 96 x 64 took 17 launches and 54 us, 25 us so.  Of 4.5 us a step the 60
+// dependent matrix instructions take 0.9; the rest is trips through LDS, transposes two bytes at a time and barriers, with
+// one wavefront per SIMD.
 //
 // Panels as in the large form; chunk c of row r of panel p lies at c ^ f(r, p), f = (r / 4) % 4, and with two halves the
 // panels take turns with hi and lo: 16 lanes that read rows, and 32 lanes that read transposing, meet different banks.
